@@ -393,6 +393,99 @@ int pdelta_patch_group(const void* W_b, const uint32_t* B_packed, const uint16_t
                        int shared_rows, void* W_out, int64_t d_out, int64_t d_in, int w_dtype,
                        void* stream);
 
+/*
+ * Layers with experts: the tokens of a call are sorted by expert and every expert has a delta (B_e, v_e) and base weights
+ * of its own (the projections of a mixture of experts), or all experts share one base (prompts for several fine-tunes of
+ * one base in one call: pdelta_linear_variants for any number of tokens of each).
+ *   offsets   in   int32 [E + 1] on the DEVICE, not decreasing: the tokens of expert e are the rows
+ *                  offsets[e] .. offsets[e + 1] - 1 of X, dY, Y and dX.  An expert may have none.  Rows before offsets[0] and
+ *                  from offsets[E] on (padding of a batch of fixed size) belong to nobody: they are not used, whatever they
+ *                  hold, and keep what they hold in Y and dX.  Nothing is read back: a call can be captured into a graph and
+ *                  replayed with other offsets.  Offsets outside 0 .. M, or that decrease, give results of no meaning for
+ *                  the experts concerned and no access outside the buffers.
+ *   W_b       in   [E, d_out, d_in], or [d_out, d_in] with shared_base = 1
+ *   B_packed  in   [E, d_out, d_in / 32] uint32
+ *   v         in   FP16 [E, d_out] (axis PDELTA_ROW) or [E, d_in] (axis PDELTA_COL)
+ *   E              1 .. 65536
+ * Everything else is as for pdelta_linear_row: dense row-major matrices, 16-byte aligned pointers (offsets too), error codes,
+ * no aliasing of outputs.  NaN and Inf in a token's row stay in that row's output.
+ * workspace: at least ..._workspace_bytes of the call, which may be 0 (then NULL is fine); PDELTA_EWORKSPACE if it is missing
+ * or smaller, PDELTA_EALIGN unless 16-byte aligned, PDELTA_EINVAL if it overlaps a tensor of the call.  Its contents on entry
+ * are ignored; it belongs to the call until the call's work on the stream has finished (two graphs that share one must not
+ * run at the same time).
+ */
+
+/*
+ * Forward: Y[m, o] = sum_i X[m, i] (W_b[e, o, i] + v B[e, o, i]) for the tokens m of every expert e.
+ *   X   in   [M, d_in], dtype x_dtype;  W_b has the same dtype
+ *   Y   out  [M, d_out], dtype y_dtype
+ * Arithmetic: weights as in pdelta_linear_row for M > 64 (one rounding of W_hat to fp16, fp32 sums, one rounding of Y); bf16
+ * tokens are multiplied as fp16 after scaling every row by a power of two, so that X has no range to stay in (elements
+ * below 2^-28 of the largest of their row lose low bits); bf16 weights must stay below 65504 in magnitude.
+ */
+size_t pdelta_linear_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype);
+
+int pdelta_linear_experts(const void* X, const int32_t* offsets, const void* W_b, int shared_base, const uint32_t* B_packed,
+                          const uint16_t* v, int axis, void* Y, int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype,
+                          int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward with respect to the input: dX[m, i] = sum_o dY[m, o] (W_b[e, o, i] + v B[e, o, i]), the gradient that goes on to the
+ * layer below.  pdelta_grad_x: one dense layer, all M tokens; W_b [d_out, d_in], v as in pdelta_linear_row / _col.
+ *   dY  in   [M, d_out], dtype (PDELTA_F16 or PDELTA_BF16), as W_b
+ *   dX  out  [M, d_in], dtype dx_dtype (PDELTA_F16, PDELTA_BF16 or PDELTA_F32)
+ * Arithmetic as in pdelta_linear_experts: bf16 gradients may be of any size, those of fp16 are what the caller's loss scale
+ * left of them.  d_out may be any number.
+ */
+size_t pdelta_grad_x_workspace_bytes(int64_t M, int64_t d_out, int64_t d_in, int dtype);
+
+int pdelta_grad_x(const void* dY, const void* W_b, const uint32_t* B_packed, const uint16_t* v, int axis, void* dX, int64_t M,
+                  int64_t d_out, int64_t d_in, int dtype, int dx_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t pdelta_grad_x_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype);
+
+int pdelta_grad_x_experts(const void* dY, const int32_t* offsets, const void* W_b, int shared_base, const uint32_t* B_packed,
+                          const uint16_t* v, int axis, void* dX, int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype,
+                          int dx_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Backward with respect to the scales, pdelta_grad_v of every expert's tokens:
+ *   row:  grad_v[e, o] = sum_m dY[m, o] * sum_i X[m, i] B[e, o, i]        over the tokens m of expert e
+ *   col:  grad_v[e, i] = sum_m X[m, i]  * sum_o dY[m, o] B[e, o, i]
+ *   grad_v  out  fp32 [E, d_out] (row) or [E, d_in] (col); overwritten; zeros for an expert without tokens
+ * Products are exact, sums are accumulated in fp32 in an order that depends on the sizes only (reproducible).  d_out may be
+ * any number in both modes.
+ */
+size_t pdelta_grad_v_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis);
+
+int pdelta_grad_v_experts(const void* X, const void* dY, const int32_t* offsets, const uint32_t* B_packed, int axis, float* grad_v,
+                          int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Loss of a student's logits against a teacher's top logits, with its gradient: what the backward calls above start from when
+ * scales are fitted end to end (the paper matches the teacher's logits; of a large vocabulary a cache holds the best few).
+ * Per token t, with z = logits / temperature, q = softmax(z) over the vocabulary and p = softmax(top_logits / temperature) over
+ * the slots that are in use:
+ *   loss[t]       = temperature^2 * weight[t] * sum_j p_j (log p_j - log q[top_ids_j])
+ *   grad[t, i]    = grad_scale * temperature * weight[t] * (q[i] - sum of the p_j with top_ids_j = i)
+ * i.e. grad = grad_scale * dloss / dlogits.
+ *   logits      in   [T, V], dtype (PDELTA_F16, PDELTA_BF16 or PDELTA_F32); -inf marks a word that is masked (q = 0)
+ *   top_ids     in   int32 [T, k]; a slot whose id is outside 0 .. V - 1 (-1, say) is not in use; one word may be named twice
+ *   top_logits  in   [T, k], dtype top_dtype (any of the three); -inf: a share of 0
+ *   weight      in   fp32 [T], or NULL for 1; a token of weight 0 gives zeros, whatever its logits are
+ *   loss        out  fp32 [T]
+ *   grad        out  [T, V], dtype; may be the same pointer as logits (the gradient replaces them); NULL: the loss alone
+ * A token without a slot in use has loss 0 and gradient 0.  Where p > 0 meets a masked word the loss is +inf and the gradient
+ * finite.  All arithmetic is in fp32; grad is rounded once.  k is 1 .. 1024, V at most 2^22, temperature > 0.
+ * T = 0 is a no-op.  workspace as above.
+ */
+size_t pdelta_distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype);
+
+int pdelta_distill(const void* logits, const int32_t* top_ids, const void* top_logits, const float* weight, float* loss, void* grad,
+                   int64_t T, int64_t V, int64_t k, int dtype, int top_dtype, float temperature, float grad_scale,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static, human-readable name of a pdelta_status value. */
 const char* pdelta_status_string(int status);
 

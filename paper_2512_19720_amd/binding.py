@@ -109,6 +109,24 @@ def lib() -> ctypes.CDLL:
         L.pdelta_linear_group_ws.argtypes = [vp, vp, vp, vp, i64, i32, vp, i64, i64, i64, i32, i32, vp, sz, vp]
         L.pdelta_patch_group.restype = i32
         L.pdelta_patch_group.argtypes = [vp, vp, vp, i64, i32, vp, i64, i64, i32, vp]
+        for name in ("pdelta_linear_experts", "pdelta_grad_x_experts"):
+            f = getattr(L, name)
+            f.restype = i32
+            f.argtypes = [vp, vp, vp, i32, vp, vp, i32, vp, i64, i64, i64, i64, i32, i32, vp, sz, vp]
+        L.pdelta_grad_x.restype = i32
+        L.pdelta_grad_x.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i32, i32, vp, sz, vp]
+        L.pdelta_grad_v_experts.restype = i32
+        L.pdelta_grad_v_experts.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, i32, vp, sz, vp]
+        for name in ("pdelta_linear_experts", "pdelta_grad_x_experts", "pdelta_grad_v_experts"):
+            f = getattr(L, name + "_workspace_bytes")
+            f.restype = sz
+            f.argtypes = [i64, i64, i64, i64, i32]
+        L.pdelta_grad_x_workspace_bytes.restype = sz
+        L.pdelta_grad_x_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.pdelta_distill_workspace_bytes.restype = sz
+        L.pdelta_distill_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.pdelta_distill.restype = i32
+        L.pdelta_distill.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i32, ctypes.c_float, ctypes.c_float, vp, sz, vp]
         L.pdelta_probe_read_stream.restype = i32
         L.pdelta_probe_read_stream.argtypes = [vp, sz, vp, vp]
         L.pdelta_probe_mfma.restype = i32
@@ -566,6 +584,169 @@ def pdelta_patch_group(W_b, B_packed, v, group: int, out=None):
                                   _dev(out, "W_out"), d_out, d_in, dtype_code(W_b.dtype), _stream())
     _check(rc, "pdelta_patch_group")
     return out
+
+
+# ---- layers with experts: tokens sorted by expert ---------------------------------------------
+# offsets is int32 [E + 1] on the GPU: the tokens of expert e are the rows offsets[e] .. offsets[e + 1] - 1.
+# W_b is [E, d_out, d_in], or [d_out, d_in] shared by all experts; B_packed [E, d_out, d_in / 32]; v [E, d_out] or [E, d_in].
+
+def _on_this_device(**tensors):
+    """Kernels go to the current device's current stream: every tensor of the call has to be there."""
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(f"{name} must be on the current GPU")
+
+
+def _call_workspace(need: int, given: torch.Tensor | None):
+    """Workspace of a call that cannot do without: the caller's own, else one of this call's."""
+    if given is None and need > 0:
+        given = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return given if given is not None and given.numel() > 0 else None
+
+
+def _expert_delta(W_b, B_packed, v, axis: int, dtype):
+    """(experts, d_out, d_in, whether they share the base weights)"""
+    if axis not in (ROW, COL):
+        raise ValueError("axis must be ROW or COL")
+    if W_b.dim() not in (2, 3) or B_packed.dim() != 3 or v.dim() != 2:
+        raise ValueError("W_b must be [E, d_out, d_in] or [d_out, d_in], B_packed [E, d_out, d_in / 32], v [E, d_out or d_in]")
+    E, (d_out, d_in) = B_packed.shape[0], W_b.shape[-2:]
+    if B_packed.shape[1] != d_out or B_packed.shape[2] * 32 != d_in or (W_b.dim() == 3 and W_b.shape[0] != E):
+        raise ValueError("W_b and B_packed must agree in experts, d_out and d_in")
+    if v.shape[0] != E or v.shape[1] != (d_out if axis == ROW else d_in):
+        raise ValueError("v must be [E, d_out] in row mode, [E, d_in] in column mode")
+    if W_b.dtype != dtype or B_packed.dtype != torch.int32 or v.dtype != torch.float16:
+        raise ValueError("W_b has the dtype of the tokens, B_packed is int32, v is float16")
+    return E, d_out, d_in, int(W_b.dim() == 2)
+
+
+def _check_offsets(offsets, E: int):
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] != E + 1:
+        raise ValueError("offsets must be int32 [E + 1]")
+
+
+def _expert_product(name: str, tokens, offsets, W_b, B_packed, v, axis: int, out, out_dtype, workspace, grad: bool):
+    if tokens.dim() != 2 or tokens.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("the tokens must be a float16 or bfloat16 matrix")
+    E, d_out, d_in, shared = _expert_delta(W_b, B_packed, v, axis, tokens.dtype)
+    width_in, width_out = (d_out, d_in) if grad else (d_in, d_out)
+    M = tokens.shape[0]
+    if tokens.shape[1] != width_in:
+        raise ValueError("the tokens and W_b must agree in " + ("d_out" if grad else "d_in"))
+    if offsets is not None:
+        _check_offsets(offsets, E)
+    if out is None:
+        out = torch.empty((M, width_out), dtype=out_dtype or tokens.dtype, device=tokens.device)
+    elif out.shape != (M, width_out) or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError("out must be one row of outputs for each token, of out_dtype")
+    _on_this_device(tokens=tokens, offsets=offsets, W_b=W_b, B_packed=B_packed, v=v, out=out, workspace=workspace)
+    L, dtype = lib(), _DTYPE_CODE[tokens.dtype]
+    need = getattr(L, f"pdelta_{'grad_x' if grad else 'linear'}_experts_workspace_bytes")(M, E, d_out, d_in, dtype)
+    ws = _call_workspace(need, workspace)
+    if offsets is None:
+        rc = L.pdelta_grad_x(_dev(tokens, "dY") or None, _dev(W_b, "W_b"), _dev(B_packed, "B_packed"), _dev(v, "v"), axis,
+                             _dev(out, "dX") or None, M, d_out, d_in, dtype, dtype_code(out.dtype), *_workspace_args(ws), _stream())
+    else:
+        rc = getattr(L, name)(_dev(tokens, "tokens") or None, _dev(offsets, "offsets"), _dev(W_b, "W_b"), shared, _dev(B_packed, "B_packed"),
+                              _dev(v, "v"), axis, _dev(out, "out") or None, M, E, d_out, d_in, dtype, dtype_code(out.dtype),
+                              *_workspace_args(ws), _stream())
+    _check(rc, name)
+    return out
+
+
+def pdelta_linear_experts_workspace_bytes(M: int, E: int, d_out: int, d_in: int, dtype: torch.dtype) -> int:
+    return int(lib().pdelta_linear_experts_workspace_bytes(M, E, d_out, d_in, dtype_code(dtype)))
+
+
+def pdelta_linear_experts(X, offsets, W_b, B_packed, v, axis: int, out=None, out_dtype=None, workspace=None):
+    """Y[m] = X[m] (W_b[e] + v[e] (.) B[e])^T for the tokens m of every expert e.
+
+    Rows that belong to no expert are not written (without ``out`` they are undefined).  ``workspace``: at least
+    ``pdelta_linear_experts_workspace_bytes`` bytes, allocated for the call unless given."""
+    return _expert_product("pdelta_linear_experts", X, offsets, W_b, B_packed, v, axis, out, out_dtype, workspace, False)
+
+
+def pdelta_grad_x_experts_workspace_bytes(M: int, E: int, d_out: int, d_in: int, dtype: torch.dtype) -> int:
+    return int(lib().pdelta_grad_x_experts_workspace_bytes(M, E, d_out, d_in, dtype_code(dtype)))
+
+
+def pdelta_grad_x_experts(dY, offsets, W_b, B_packed, v, axis: int, out=None, out_dtype=None, workspace=None):
+    """dX[m] = dY[m] (W_b[e] + v[e] (.) B[e]) for the tokens m of every expert e; the rest as in ``pdelta_linear_experts``."""
+    return _expert_product("pdelta_grad_x_experts", dY, offsets, W_b, B_packed, v, axis, out, out_dtype, workspace, True)
+
+
+def pdelta_grad_x_workspace_bytes(M: int, d_out: int, d_in: int, dtype: torch.dtype) -> int:
+    return int(lib().pdelta_grad_x_workspace_bytes(M, d_out, d_in, dtype_code(dtype)))
+
+
+def pdelta_grad_x(dY, W_b, B_packed, v, axis: int, out=None, out_dtype=None, workspace=None):
+    """dX = dY (W_b + v (.) B): the gradient with respect to the input of one dense layer."""
+    if W_b.dim() != 2 or B_packed.dim() != 2 or v.dim() != 1:
+        raise ValueError("W_b must be [d_out, d_in], B_packed [d_out, d_in / 32], v [d_out] or [d_in]")
+    return _expert_product("pdelta_grad_x", dY, None, W_b, B_packed.unsqueeze(0), v.unsqueeze(0), axis, out, out_dtype, workspace, True)
+
+
+def pdelta_grad_v_experts_workspace_bytes(M: int, E: int, d_out: int, d_in: int, axis: int) -> int:
+    return int(lib().pdelta_grad_v_experts_workspace_bytes(M, E, d_out, d_in, axis))
+
+
+def pdelta_grad_v_experts(X, dY, offsets, B_packed, axis: int, out=None, workspace=None):
+    """dL/dv (fp32) of every expert's tokens for upstream gradient dY: [E, d_out] in row mode, [E, d_in] in column mode;
+    zeros for an expert without tokens."""
+    if axis not in (ROW, COL):
+        raise ValueError("axis must be ROW or COL")
+    if X.dim() != 2 or dY.dim() != 2 or dY.shape[0] != X.shape[0] or dY.dtype != X.dtype:
+        raise ValueError("X and dY must agree in M and dtype")
+    (M, d_in), d_out = X.shape, dY.shape[1]
+    if B_packed.dim() != 3 or B_packed.dtype != torch.int32 or B_packed.shape[1] != d_out or B_packed.shape[2] * 32 != d_in:
+        raise ValueError("B_packed must be int32 [E, d_out, d_in / 32]")
+    E, kept = B_packed.shape[0], d_out if axis == ROW else d_in
+    _check_offsets(offsets, E)
+    if out is None:
+        out = torch.empty((E, kept), dtype=torch.float32, device=X.device)
+    elif out.shape != (E, kept) or out.dtype != torch.float32:
+        raise ValueError("out must be float32 [E, d_out] in row mode, [E, d_in] in column mode")
+    _on_this_device(X=X, dY=dY, offsets=offsets, B_packed=B_packed, out=out, workspace=workspace)
+    ws = _call_workspace(pdelta_grad_v_experts_workspace_bytes(M, E, d_out, d_in, axis), workspace)
+    rc = lib().pdelta_grad_v_experts(_dev(X, "X") or None, _dev(dY, "dY") or None, _dev(offsets, "offsets"), _dev(B_packed, "B_packed"),
+                                     axis, _dev(out, "grad_v"), M, E, d_out, d_in, dtype_code(X.dtype), *_workspace_args(ws), _stream())
+    _check(rc, "pdelta_grad_v_experts")
+    return out
+
+
+# ---- loss against a teacher's top logits ------------------------------------------------------
+
+def pdelta_distill_workspace_bytes(T: int, V: int, k: int, dtype: torch.dtype) -> int:
+    return int(lib().pdelta_distill_workspace_bytes(T, V, k, dtype_code(dtype)))
+
+
+def pdelta_distill(logits, top_ids, top_logits, weight=None, temperature: float = 1.0, grad_scale: float = 1.0, want_grad: bool = True,
+                   out=None, workspace=None):
+    """(loss fp32 [T], grad [T, V] | None): temperature^2 weight KL(teacher's top words || student) of every token, and
+    grad_scale times its gradient with respect to the logits.
+
+    ``top_ids`` int32 [T, k] (a slot with an id outside 0 .. V - 1 is not in use), ``top_logits`` [T, k], ``weight`` fp32 [T].
+    ``out``: the gradient's buffer, ``logits`` itself if the gradient may replace them."""
+    if logits.dim() != 2 or top_ids.dim() != 2 or top_ids.shape[0] != logits.shape[0] or top_logits.shape != top_ids.shape:
+        raise ValueError("logits must be [T, V], top_ids and top_logits [T, k]")
+    (T, V), k = logits.shape, top_ids.shape[1]
+    if top_ids.dtype != torch.int32:
+        raise ValueError("top_ids must be int32")
+    if weight is not None and (weight.shape != (T,) or weight.dtype != torch.float32):
+        raise ValueError("weight must be float32 [T]")
+    if out is not None and (not want_grad or out.shape != logits.shape or out.dtype != logits.dtype):
+        raise ValueError("out is the gradient's buffer, like logits")
+    if want_grad and out is None:
+        out = torch.empty_like(logits)
+    loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+    _on_this_device(logits=logits, top_ids=top_ids, top_logits=top_logits, weight=weight, out=out, workspace=workspace)
+    ws = _call_workspace(pdelta_distill_workspace_bytes(T, V, k, logits.dtype), workspace)
+    rc = lib().pdelta_distill(_dev(logits, "logits") or None, _dev(top_ids, "top_ids") or None, _dev(top_logits, "top_logits") or None,
+                              _dev(weight, "weight") if weight is not None else None, _dev(loss, "loss") or None,
+                              (_dev(out, "grad") or None) if out is not None else None, T, V, k, dtype_code(logits.dtype),
+                              dtype_code(top_logits.dtype), temperature, grad_scale, *_workspace_args(ws), _stream())
+    _check(rc, "pdelta_distill")
+    return loss, out
 
 
 # ---- bench helpers (include/pdelta_probes.h): what this GPU sustains, not part of the method ----

@@ -7,6 +7,8 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
+#include <initializer_list>
 
 #include "pdelta_host.h"
 
@@ -686,6 +688,187 @@ int pdelta_patch_group(const void* W_b, const uint32_t* B_packed, const uint16_t
     const int rc = launch_patch_group(w_dtype, W_b, B_packed, v, W_out, d_out, d_in, v_stride, g_shift,
                                       (hipStream_t)stream);
     return rc == 0 ? PDELTA_OK : PDELTA_EHIP;
+}
+
+// ---- tokens sorted by expert -------------------------------------------------------------------
+
+namespace pdelta {
+namespace {
+
+constexpr int64_t kMaxExperts = 1 << 16, kMaxWords = 1024;
+
+struct Buffer { const void* p; size_t bytes; };
+
+// The output (and a workspace) apart from every input and from each other.
+int check_apart(Buffer out, Buffer workspace, std::initializer_list<Buffer> inputs)
+{
+    for (const Buffer& in : inputs) {
+        if (in.bytes == 0) continue;
+        if (overlaps(out.p, out.bytes, in.p, in.bytes)) return PDELTA_EINVAL;
+        if (workspace.bytes != 0 && overlaps(workspace.p, workspace.bytes, in.p, in.bytes)) return PDELTA_EINVAL;
+    }
+    return workspace.bytes != 0 && overlaps(out.p, out.bytes, workspace.p, workspace.bytes) ? PDELTA_EINVAL : PDELTA_OK;
+}
+
+int check_workspace(const void* workspace, size_t workspace_bytes, size_t need)
+{
+    if (workspace == nullptr && workspace_bytes != 0) return PDELTA_EINVAL;
+    if (workspace_bytes < need) return PDELTA_EWORKSPACE;
+    return misaligned(workspace) ? PDELTA_EALIGN : PDELTA_OK;
+}
+
+int check_experts(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
+{
+    if (axis != PDELTA_ROW && axis != PDELTA_COL) return PDELTA_EINVAL;
+    if (M < 0 || E < 1) return PDELTA_EINVAL;
+    if (const int rc = check_dims(d_out, d_in)) return rc;
+    return M > kMaxTokens || E > kMaxExperts ? PDELTA_ESHAPE : PDELTA_OK;
+}
+
+// Forward (grad = false: tokens X, out Y) and backward with respect to the input (tokens dY, out dX).
+int experts_product(const ExpertsCall& call, bool grad, bool dense, int shared_base, size_t workspace_bytes, void* stream)
+{
+    const TuneScope tune_scope;
+    ExpertsCall c = call;
+    if (c.W_b == nullptr || c.B_packed == nullptr || c.v == nullptr || (!dense && c.offsets == nullptr)) return PDELTA_EINVAL;
+    if (shared_base != 0 && shared_base != 1) return PDELTA_EINVAL;
+    if (const int rc = check_experts(c.M, c.E, c.d_out, c.d_in, c.axis)) return rc;
+    if (c.M > 0 && (c.tokens == nullptr || c.out == nullptr)) return PDELTA_EINVAL;
+    if (!is_w_dtype(c.dtype) || !is_y_dtype(c.out_dtype)) return PDELTA_EDTYPE;
+    if (misaligned(c.tokens) || misaligned(c.offsets) || misaligned(c.W_b) || misaligned(c.B_packed) || misaligned(c.v) || misaligned(c.out))
+        return PDELTA_EALIGN;
+    const size_t need = grad ? experts_grad_x_workspace_bytes(c.M, c.E, c.d_out, c.d_in, c.dtype)
+                             : experts_linear_workspace_bytes(c.M, c.E, c.d_out, c.d_in, c.dtype);
+    if (const int rc = check_workspace(c.workspace, workspace_bytes, need)) return rc;
+    if (c.M == 0) return PDELTA_OK;
+    const size_t layer = (size_t)c.d_out * c.d_in, E = (size_t)c.E;
+    const size_t in_width = (size_t)(grad ? c.d_out : c.d_in), out_width = (size_t)(grad ? c.d_in : c.d_out);
+    if (const int rc = check_apart({c.out, (size_t)c.M * out_width * (c.out_dtype == PDELTA_F32 ? 4 : 2)}, {c.workspace, workspace_bytes},
+                                   {{c.tokens, (size_t)c.M * in_width * 2}, {c.offsets, dense ? 0 : (E + 1) * 4},
+                                    {c.W_b, (shared_base ? 1 : E) * layer * 2}, {c.B_packed, E * layer / 8},
+                                    {c.v, E * (size_t)(c.axis == PDELTA_ROW ? c.d_out : c.d_in) * 2}}))
+        return rc;
+    c.w_stride = shared_base ? 0 : (int64_t)layer;
+    const int rc = grad ? launch_experts_grad_x(c, (hipStream_t)stream) : launch_experts_linear(c, (hipStream_t)stream);
+    return rc == 0 ? PDELTA_OK : rc == -2 ? PDELTA_ESHAPE : PDELTA_EHIP;
+}
+
+}  // namespace
+}  // namespace pdelta
+
+static bool experts_sizes_ok(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
+{
+    return pdelta::check_experts(M, E, d_out, d_in, axis) == PDELTA_OK;
+}
+
+size_t pdelta_linear_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype)
+{
+    const pdelta::TuneScope tune_scope;
+    if (!experts_sizes_ok(M, E, d_out, d_in, PDELTA_ROW) || !pdelta::is_w_dtype(x_dtype)) return 0;
+    return pdelta::experts_linear_workspace_bytes(M, E, d_out, d_in, x_dtype);
+}
+
+int pdelta_linear_experts(const void* X, const int32_t* offsets, const void* W_b, int shared_base, const uint32_t* B_packed,
+                          const uint16_t* v, int axis, void* Y, int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype,
+                          int y_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return pdelta::experts_product({X, offsets, W_b, 0, B_packed, v, Y, M, E, d_out, d_in, axis, x_dtype, y_dtype, workspace}, false, false,
+                                   shared_base, workspace_bytes, stream);
+}
+
+size_t pdelta_grad_x_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
+{
+    const pdelta::TuneScope tune_scope;
+    if (!experts_sizes_ok(M, E, d_out, d_in, PDELTA_ROW) || !pdelta::is_w_dtype(dtype)) return 0;
+    return pdelta::experts_grad_x_workspace_bytes(M, E, d_out, d_in, dtype);
+}
+
+int pdelta_grad_x_experts(const void* dY, const int32_t* offsets, const void* W_b, int shared_base, const uint32_t* B_packed,
+                          const uint16_t* v, int axis, void* dX, int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype,
+                          int dx_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return pdelta::experts_product({dY, offsets, W_b, 0, B_packed, v, dX, M, E, d_out, d_in, axis, dtype, dx_dtype, workspace}, true, false,
+                                   shared_base, workspace_bytes, stream);
+}
+
+size_t pdelta_grad_x_workspace_bytes(int64_t M, int64_t d_out, int64_t d_in, int dtype)
+{
+    return pdelta_grad_x_experts_workspace_bytes(M, 1, d_out, d_in, dtype);
+}
+
+int pdelta_grad_x(const void* dY, const void* W_b, const uint32_t* B_packed, const uint16_t* v, int axis, void* dX, int64_t M,
+                  int64_t d_out, int64_t d_in, int dtype, int dx_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return pdelta::experts_product({dY, nullptr, W_b, 0, B_packed, v, dX, M, 1, d_out, d_in, axis, dtype, dx_dtype, workspace}, true, true, 1,
+                                   workspace_bytes, stream);
+}
+
+size_t pdelta_grad_v_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
+{
+    const pdelta::TuneScope tune_scope;
+    if (!experts_sizes_ok(M, E, d_out, d_in, axis)) return 0;
+    return pdelta::experts_grad_v_workspace_bytes(M, E, d_out, d_in, axis);
+}
+
+int pdelta_grad_v_experts(const void* X, const void* dY, const int32_t* offsets, const uint32_t* B_packed, int axis, float* grad_v,
+                          int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype, void* workspace, size_t workspace_bytes,
+                          void* stream)
+{
+    using namespace pdelta;
+    const TuneScope tune_scope;
+    if (offsets == nullptr || B_packed == nullptr || grad_v == nullptr) return PDELTA_EINVAL;
+    if (const int rc = check_experts(M, E, d_out, d_in, axis)) return rc;
+    if (M > 0 && (X == nullptr || dY == nullptr)) return PDELTA_EINVAL;
+    if (!is_w_dtype(dtype)) return PDELTA_EDTYPE;
+    if (misaligned(X) || misaligned(dY) || misaligned(offsets) || misaligned(B_packed) || misaligned(grad_v)) return PDELTA_EALIGN;
+    if (const int rc = check_workspace(workspace, workspace_bytes, experts_grad_v_workspace_bytes(M, E, d_out, d_in, axis))) return rc;
+    if (const int rc = check_apart({grad_v, (size_t)E * (axis == PDELTA_ROW ? d_out : d_in) * 4}, {workspace, workspace_bytes},
+                                   {{X, (size_t)M * d_in * 2}, {dY, (size_t)M * d_out * 2}, {offsets, (size_t)(E + 1) * 4},
+                                    {B_packed, (size_t)E * d_out * d_in / 8}}))
+        return rc;
+    const int rc = launch_experts_grad_v(dtype, axis, X, dY, offsets, B_packed, grad_v, M, E, d_out, d_in, workspace, (hipStream_t)stream);
+    return rc == 0 ? PDELTA_OK : rc == -2 ? PDELTA_ESHAPE : PDELTA_EHIP;
+}
+
+// ---- loss against a teacher's top logits -------------------------------------------------------
+
+static int distill_sizes(int64_t T, int64_t V, int64_t k)
+{
+    using namespace pdelta;
+    if (T < 0 || V < 1 || k < 1) return PDELTA_EINVAL;
+    return T > kMaxTokens || V > kMaxDim || k > kMaxWords ? PDELTA_ESHAPE : PDELTA_OK;
+}
+
+size_t pdelta_distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype)
+{
+    const pdelta::TuneScope tune_scope;
+    if (distill_sizes(T, V, k) != PDELTA_OK || !pdelta::is_y_dtype(dtype)) return 0;
+    return pdelta::distill_workspace_bytes(T, V, k, dtype);
+}
+
+int pdelta_distill(const void* logits, const int32_t* top_ids, const void* top_logits, const float* weight, float* loss, void* grad,
+                   int64_t T, int64_t V, int64_t k, int dtype, int top_dtype, float temperature, float grad_scale,
+                   void* workspace, size_t workspace_bytes, void* stream)
+{
+    using namespace pdelta;
+    const TuneScope tune_scope;
+    if (const int rc = distill_sizes(T, V, k)) return rc;
+    if (T > 0 && (logits == nullptr || top_ids == nullptr || top_logits == nullptr || loss == nullptr)) return PDELTA_EINVAL;
+    if (!(temperature >= 1e-6f && temperature <= 1e6f) || !std::isfinite(grad_scale)) return PDELTA_EINVAL;
+    if (!is_y_dtype(dtype) || !is_y_dtype(top_dtype)) return PDELTA_EDTYPE;
+    if (misaligned(logits) || misaligned(top_ids) || misaligned(top_logits) || misaligned(weight) || misaligned(loss) || misaligned(grad))
+        return PDELTA_EALIGN;
+    if (const int rc = check_workspace(workspace, workspace_bytes, pdelta::distill_workspace_bytes(T, V, k, dtype))) return rc;
+    if (T == 0) return PDELTA_OK;
+    const size_t bytes = (size_t)T * V * (dtype == PDELTA_F32 ? 4 : 2);
+    const Buffer in_logits{logits, bytes}, in_ids{top_ids, (size_t)T * k * 4}, in_top{top_logits, (size_t)T * k * (top_dtype == PDELTA_F32 ? 4 : 2)},
+                 in_weight{weight, weight != nullptr ? (size_t)T * 4 : 0}, out_loss{loss, (size_t)T * 4}, out_grad{grad, grad != nullptr ? bytes : 0};
+    if (const int rc = check_apart(out_loss, {workspace, workspace_bytes}, {in_logits, in_ids, in_top, in_weight, out_grad})) return rc;
+    if (grad != nullptr)
+        if (const int rc = check_apart(out_grad, {nullptr, 0}, {grad == logits ? Buffer{nullptr, 0} : in_logits, in_ids, in_top, in_weight})) return rc;
+    const int rc = launch_distill({logits, top_ids, top_logits, weight, loss, grad, T, V, k, dtype, top_dtype, temperature, grad_scale, workspace},
+                                  (hipStream_t)stream);
+    return rc == 0 ? PDELTA_OK : rc == -2 ? PDELTA_ESHAPE : PDELTA_EHIP;
 }
 
 const char* pdelta_status_string(int status)

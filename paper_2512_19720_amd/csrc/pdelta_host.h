@@ -134,6 +134,47 @@ int launch_linear_gemm_parts(int parts, int y_dtype, const void* X, const void* 
                              const uint16_t* v, void* Y, int64_t M, int64_t d_out, int64_t d_in,
                              hipStream_t stream);
 
+// Tokens sorted by expert (offsets: E + 1 row numbers on the device).  w_stride: weights between two experts' W_b, 0 when they
+// share one.  tokens, out: X and Y, or dY and dX.
+struct ExpertsCall {
+    const void* tokens;
+    const int* offsets;
+    const void* W_b;
+    int64_t w_stride;
+    const uint32_t* B_packed;
+    const uint16_t* v;
+    void* out;
+    int64_t M, E, d_out, d_in;
+    int axis, dtype, out_dtype;
+    void* workspace;
+};
+// Products with W_hat, and with its transpose.  These and the following return -2 where a grid would be too large.
+size_t experts_linear_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype);
+size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype);
+int launch_experts_linear(const ExpertsCall& c, hipStream_t stream);
+int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream);
+
+// Gradient with respect to every expert's scales.
+size_t experts_grad_v_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis);
+int launch_experts_grad_v(int dtype, int axis, const void* X, const void* dY, const int* offsets, const uint32_t* B_packed, float* grad,
+                          int64_t M, int64_t E, int64_t d_out, int64_t d_in, void* workspace, hipStream_t stream);
+
+// Loss against a teacher's top logits, and its gradient.
+struct DistillCall {
+    const void* logits;
+    const int* ids;
+    const void* top;
+    const float* weight;
+    float* loss;
+    void* grad;
+    int64_t T, V, k;
+    int dtype, top_dtype;
+    float temperature, grad_scale;
+    void* workspace;
+};
+size_t distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype);
+int launch_distill(const DistillCall& c, hipStream_t stream);
+
 // Integer tuning knobs from the environment variable PDELTA_TUNE ("key=value,key=value");
 // returns `fallback` when the key is absent.  Every C-ABI entry point that launches opens a
 // TuneScope, which reads the variable once for the whole call.

@@ -1,0 +1,187 @@
+"""GPU: products of tokens sorted by expert, forward and backward, and the gradient of every expert's scales, against the
+64-bit forms of experts_util with its bounds."""
+import pytest
+import torch
+
+from experts_util import COL, ROW, grad_v64, held, product64
+from paper_2512_19720_amd import binding as pd
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def make(counts, d_out, d_in, dtype, axis, seed, shared=False, before=0, behind=0, dy_scale=1e-3):
+    g = torch.Generator().manual_seed(seed)
+    E, M = len(counts), before + sum(counts) + behind
+    offsets = [before]
+    for n in counts:
+        offsets.append(offsets[-1] + n)
+    c = {"offsets": torch.tensor(offsets, dtype=torch.int32),
+         "B": torch.randint(-2 ** 31, 2 ** 31, (E, d_out, d_in // 32), generator=g).to(torch.int32),
+         "W_b": (torch.randn((d_out, d_in) if shared else (E, d_out, d_in), generator=g) * 0.02).to(dtype),
+         "v": (torch.randn(E, d_out if axis == ROW else d_in, generator=g) * 1e-3).to(F16),          # of either sign
+         "X": torch.randn(M, d_in, generator=g).to(dtype),
+         "dY": (torch.randn(M, d_out, generator=g) * dy_scale * torch.exp(torch.randn(M, 1, generator=g))).to(dtype)}
+    return {k: t.to(DEV) for k, t in c.items()}
+
+
+def linear(c, axis, out_dtype, **kw):
+    return pd.pdelta_linear_experts(c["X"], c["offsets"], c["W_b"], c["B"], c["v"], axis, out_dtype=out_dtype, **kw)
+
+
+def grad_x(c, axis, out_dtype, **kw):
+    return pd.pdelta_grad_x_experts(c["dY"], c["offsets"], c["W_b"], c["B"], c["v"], axis, out_dtype=out_dtype, **kw)
+
+
+def check_products(c, axis, out_dtype, what):
+    for grad, name, tokens in ((False, "linear", c["X"]), (True, "grad_x", c["dY"])):
+        width = c["W_b"].shape[-1 if grad else -2]
+        out = torch.full((tokens.shape[0], width), 7.0, dtype=out_dtype, device=DEV)
+        (grad_x if grad else linear)(c, axis, out_dtype, out=out)
+        ref, bound, mine = product64(tokens, c["offsets"], c["W_b"], c["B"], c["v"], axis, grad, out_dtype)
+        held(out.cpu()[mine], ref[mine], bound[mine], f"{name} {what}")
+        assert (out.cpu()[~mine] == 7.0).all(), f"{name} {what}: a row that belongs to nobody was written"
+
+
+# (tokens of each expert, d_out, d_in): none and one, tiles and their edges, outputs that are no multiple of anything, inputs
+# that are one of 32 only, many experts with few tokens
+SHAPES = [([1], 32, 32), ([0, 3, 0, 1], 65, 96), ([5, 0, 64, 65], 130, 160), ([63, 1, 17], 257, 128), ([2] * 70, 48, 256),
+          ([130, 0, 257], 300, 384), ([0, 0, 0], 40, 64), ([300], 129, 544), ([16, 17, 15, 1, 0, 33], 272, 640), ([40, 3], 1001, 1056)]
+
+
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("counts,d_out,d_in", SHAPES)
+def test_products_match(counts, d_out, d_in, dtype, axis):
+    c = make(counts, d_out, d_in, dtype, axis, 100 + d_out + d_in, before=d_out % 3, behind=d_in // 32 % 4)
+    for out_dtype in (dtype, F32):
+        check_products(c, axis, out_dtype, f"{counts} {d_out}x{d_in} {dtype} axis {axis} -> {out_dtype}")
+
+
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("counts,d_out,d_in", SHAPES)
+def test_grad_v_matches(counts, d_out, d_in, dtype, axis):
+    c = make(counts, d_out, d_in, dtype, axis, 200 + d_out + d_in, before=2, behind=3)
+    c["X"][:2], c["X"][-3:], c["dY"][:2], c["dY"][-3:] = float("nan"), float("inf"), float("nan"), float("nan")    # nobody's rows
+    got = pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis)
+    ref, bound = grad_v64(c["X"].nan_to_num(0, 0, 0), c["dY"].nan_to_num(0, 0, 0), c["offsets"], c["B"], axis)
+    held(got, ref, bound, f"grad_v {counts} {d_out}x{d_in} {dtype} axis {axis}")
+    again = pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis)
+    assert torch.equal(got, again)                    # sums in a fixed order
+
+
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_shared_base(dtype, axis):
+    c = make([70, 0, 9, 33], 192, 256, dtype, axis, 5, shared=True)
+    check_products(c, axis, dtype, f"shared base {dtype} axis {axis}")
+
+
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,d_out,d_in", [(1, 33, 64), (77, 320, 256), (200, 1001, 352)])
+def test_dense_grad_x(M, d_out, d_in, dtype, axis):
+    c = make([M], d_out, d_in, dtype, axis, 6, shared=True)
+    got = pd.pdelta_grad_x(c["dY"], c["W_b"], c["B"][0], c["v"][0], axis)
+    ref, bound, _ = product64(c["dY"], c["offsets"], c["W_b"], c["B"], c["v"], axis, True, dtype)
+    held(got, ref, bound, f"dense grad_x {M} {d_out}x{d_in}")
+    assert torch.equal(got, grad_x(c, axis, dtype))   # one expert with all tokens
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e-6, 1e6, 1e30])
+def test_bf16_gradients_of_any_size(scale):
+    """Far below and far above what fp16 holds; rows of zeros among them."""
+    c = make([65, 7], 160, 128, BF16, ROW, 8, dy_scale=scale)
+    c["dY"][3], c["dY"][70] = 0, 0
+    got = grad_x(c, ROW, F32)
+    ref, bound, _ = product64(c["dY"], c["offsets"], c["W_b"], c["B"], c["v"], ROW, True, F32)
+    held(got, ref, bound, f"gradients of {scale}")
+    assert not got[3].any() and not got[70].any()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_what_is_not_a_number_stays_in_its_row(dtype):
+    c = make([40, 30], 96, 128, dtype, COL, 9, behind=2)
+    clean_y, clean_x = linear(c, COL, dtype), grad_x(c, COL, dtype)
+    for t in (c["X"], c["dY"]):
+        t[5, 3], t[50, 7], t[70:] = float("nan"), float("inf"), float("nan")
+    for got, clean in ((linear(c, COL, dtype), clean_y), (grad_x(c, COL, dtype), clean_x)):
+        others = [m for m in range(70) if m not in (5, 50)]
+        assert torch.equal(got[others], clean[others])
+        assert got[5].isnan().all() and not got[50].isfinite().any()
+
+
+def test_offsets_out_of_order_stay_in_bounds():
+    """No meaning, but no access outside the buffers: the guards around the outputs hold."""
+    c = make([40, 30, 20], 96, 128, BF16, ROW, 10)
+    for offsets in ([0, 500, 20, 90], [-7, 10, 90, 90], [90, 40, 20, 0], [2 ** 31 - 1, -2 ** 31, 50, 2 ** 31 - 1]):
+        c["offsets"] = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+        pad = torch.full((90 + 40, 96), 7.0, dtype=BF16, device=DEV)
+        linear(c, ROW, BF16, out=pad[20:110])
+        assert (pad[:20] == 7.0).all() and (pad[110:] == 7.0).all()
+        padx = torch.full((90 + 40, 128), 7.0, dtype=BF16, device=DEV)
+        grad_x(c, ROW, BF16, out=padx[20:110])
+        assert (padx[:20] == 7.0).all() and (padx[110:] == 7.0).all()
+        assert pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], ROW).shape == (3, 96)
+
+
+def test_no_tokens():
+    c = make([0, 0], 64, 96, F16, ROW, 11)
+    assert linear(c, ROW, F16).shape == (0, 64) and grad_x(c, ROW, F16).shape == (0, 96)
+    out = torch.full((2, 64), 3.0, device=DEV)
+    pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], ROW, out=out)
+    assert not out.any()
+
+
+def test_one_expert_is_the_dense_layer():
+    """Against the library's own dense calls: the same weights, one expert."""
+    c = make([150], 256, 256, F16, ROW, 12, shared=True)
+    Y = pd.pdelta_linear_row(c["X"], c["W_b"], c["B"][0], c["v"][0], out_dtype=F32)
+    ref, bound, _ = product64(c["X"], c["offsets"], c["W_b"], c["B"], c["v"], ROW, False, F32)
+    held(Y, ref, bound, "dense")
+    held(linear(c, ROW, F32), ref, bound, "one expert")
+    g = pd.pdelta_grad_v(c["X"], c["dY"], c["B"][0], ROW)
+    held(g[None], *grad_v64(c["X"], c["dY"], c["offsets"], c["B"], ROW), "dense grad_v")
+
+
+def test_another_stream():
+    c = make([64, 40], 128, 256, BF16, COL, 13)
+    want = [linear(c, COL, BF16), grad_x(c, COL, BF16), pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], COL)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [linear(c, COL, BF16), grad_x(c, COL, BF16), pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], COL)]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_captured_call_follows_the_offsets(dtype):
+    """One graph of the three calls, replayed with other tokens and other shares of the experts."""
+    axis, M, E = ROW, 96, 3
+    c = make([50, 0, 46], 130, 256, dtype, axis, 14)
+    def calls():
+        return linear(c, axis, dtype), grad_x(c, axis, dtype), pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held_out = calls()
+    for k, offsets in enumerate(([0, 50, 50, 96], [0, 96, 96, 96], [0, 1, 33, 96], [0, 0, 0, 96])):
+        fresh = make([50, 0, 46], 130, 256, dtype, axis, 20 + k)
+        for name in ("X", "dY"):
+            c[name].copy_(fresh[name])
+        c["offsets"].copy_(torch.tensor(offsets, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held_out]
+        for a, b in zip(got, calls()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
