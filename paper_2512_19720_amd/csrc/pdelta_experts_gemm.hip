@@ -18,8 +18,6 @@
 
 namespace pdelta {
 
-constexpr int kPrepUnit = 128;                        // rows of the prepared operand are padded with zeros to a multiple
-
 // One workgroup per row.  Reads the row twice (the second time out of the cache), writes it once.
 template <int DT>
 __global__ void __launch_bounds__(256)
@@ -167,14 +165,19 @@ experts_tile_kernel(const uint16_t* __restrict__ A, int lda, const float* __rest
     }
 }
 
+void launch_experts_copy_rows(const void* rows, void* out, int64_t M, int64_t K, hipStream_t stream)
+{
+    hipLaunchKernelGGL(experts_prepare_kernel<kF16>, dim3((unsigned)M), dim3(256), 0, stream, (const uint16_t*)rows, (uint16_t*)out, nullptr,
+                       (int)K, (int)experts_padded(K));
+}
+
 // The prepared token operand: fp16 rows of `lda` values, behind them an fp32 factor for each row.
-static int64_t prepared_lda(int64_t K) { return (K + kPrepUnit - 1) / kPrepUnit * kPrepUnit; }
 static bool needs_prepare(int64_t K, int dtype) { return dtype == kBF16 || (K & 7) != 0; }
 
 static size_t prepared_bytes(int64_t M, int64_t K, int dtype)
 {
     if (!needs_prepare(K, dtype)) return 0;
-    return (size_t)M * (size_t)prepared_lda(K) * 2 + ((size_t)M * 4 + 15) / 16 * 16;
+    return (size_t)M * (size_t)experts_padded(K) * 2 + ((size_t)M * 4 + 15) / 16 * 16;
 }
 
 template <int WDT, int AXIS, bool GRAD>
@@ -197,14 +200,14 @@ static int launch_product(const ExpertsCall& c, bool grad, hipStream_t stream)
     const float* inverse = nullptr;
     int lda = (int)K;
     if (needs_prepare(K, c.dtype)) {
-        lda = (int)prepared_lda(K);
+        lda = (int)experts_padded(K);
         uint16_t* rows = (uint16_t*)c.workspace;
         float* factors = (float*)(rows + c.M * lda);
         if (c.dtype == kBF16) {
             hipLaunchKernelGGL(experts_prepare_kernel<kBF16>, dim3((unsigned)c.M), dim3(256), 0, stream, A, rows, factors, (int)K, lda);
             inverse = factors;
         } else {
-            hipLaunchKernelGGL(experts_prepare_kernel<kF16>, dim3((unsigned)c.M), dim3(256), 0, stream, A, rows, factors, (int)K, lda);
+            launch_experts_copy_rows(A, rows, c.M, K, stream);
         }
         A = rows;
     }

@@ -9,7 +9,7 @@
 
 #include "pdelta_experts.h"
 #include "pdelta_host.h"
-#include "pdelta_skinny_tile.h"
+#include "pdelta_lds_load.h"
 
 namespace pdelta {
 
@@ -22,67 +22,190 @@ __device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c)
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
 
-// The general tile: 64 of the summed dimension x 64 of the kept one, steps of 64 tokens, 4 waves of 32 x 32.
-constexpr int kGradTile = 64, kGradTokens = 64, kGradLD = kGradTokens + 8;
+// Tiles of 256 of the summed dimension (P) x 256 of the kept one (Q), 8 waves of 128 x 64, steps of 64 tokens, two stages in
+// LDS filled by direct loads.  Both operands lie in memory with the tokens as rows, and the contraction runs over the tokens:
+// the fragments are read from LDS by transposing reads, 4 tokens x 16 columns for 16 lanes.
+constexpr int kGradTile = 256, kGradTokens = 64;
+constexpr int kGradOperand = kGradTokens * kGradTile * 2, kGradStage = 2 * kGradOperand, kGradLds = 2 * kGradStage;
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+// Four values of one column from 16 lanes' rows of four: lane 4 r + c of 16 points at columns 4 c .. 4 c + 3 of row r, lane i gets
+// rows 0 .. 3 of column i.
+__device__ __forceinline__ uint2v read_transposed(const unsigned char* p)
+{
+    return __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)p));
+}
 
 template <int DT, int AXIS>
-__global__ void __launch_bounds__(256)
-experts_grad_kernel(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, const int* __restrict__ offsets,
+__global__ void __launch_bounds__(512, 2)
+experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __restrict__ dY, int y_ld, const int* __restrict__ offsets,
                     const uint32_t* __restrict__ B_packed, float* __restrict__ partial, int M, int d_out, int d_in, int kept_tiles,
                     int sum_tiles)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t Ps[kGradTile * kGradLD], Qs[kGradTile * kGradLD];
-    __shared__ float red[2][kGradTile];
+    constexpr int FP = 4, FQ = 2;
+    extern __shared__ __attribute__((aligned(16))) unsigned char grad_smem[];
     const int kt = blockIdx.x % kept_tiles, st = blockIdx.x / kept_tiles % sum_tiles, e = blockIdx.x / kept_tiles / sum_tiles;
     int first, end;
     expert_rows(offsets, e, M, first, end);
     if (first == end) return;                         // whole workgroup
-    const uint16_t* P = AXIS == 0 ? X : dY;           // summed dimension
-    const uint16_t* Q = AXIS == 0 ? dY : X;           // kept dimension
     const int dP = AXIS == 0 ? d_in : d_out, dQ = AXIS == 0 ? d_out : d_in;
-    const int p0 = st * kGradTile, q0 = kt * kGradTile;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int p_ld = AXIS == 0 ? x_ld : y_ld, q_ld = AXIS == 0 ? y_ld : x_ld;
+    const int p0 = st * kGradTile, q0 = kt * kGradTile, words = d_in / 32;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wp = wave >> 2, wq = wave & 3;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)grad_smem;
+    const uint32_t* signs = B_packed + (int64_t)e * d_out * words;
 
-    // [token][column] -> LDS [column][token]; what is behind the expert's tokens or the matrix is zero
-    auto stage = [&](const uint16_t* src, int width, int c0, int m0, uint16_t* lds) {
-        for (int c = tid; c < kGradTile * kGradTokens; c += 256) {
-            const int col = c % kGradTile, tok = c / kGradTile;
-            lds[col * kGradLD + tok] = m0 + tok < end && c0 + col < width ? src[(int64_t)(m0 + tok) * width + c0 + col] : 0;
+    // The signs of the tile, asked for before everything else.  Row mode (P are inputs, Q outputs): the lane's output row h holds
+    // the wave's 128 inputs in four words.  Column mode: a thread brings half a row of the tile to LDS in the end.
+    uint32_t sw[FQ][FP];
+    if constexpr (AXIS == 0) {
+#pragma unroll
+        for (int h = 0; h < FQ; ++h)
+#pragma unroll
+            for (int f = 0; f < FP; ++f)
+                sw[h][f] = signs[(int64_t)min(q0 + wq * 64 + h * 32 + (lane & 31), d_out - 1) * words + min(p0 / 32 + wp * 4 + f, words - 1)];
+    } else {
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+            sw[0][f] = signs[(int64_t)min(p0 + (int)threadIdx.x / 2, d_out - 1) * words + min(q0 / 32 + ((int)threadIdx.x & 1) * 4 + f, words - 1)];
+    }
+
+    // One load instruction brings 512 bytes of two tokens; a wave brings 8 tokens of each operand.  The 16-byte piece c of token t
+    // goes to place c ^ 4 (t & 3), so that the four tokens of a transposing read are in different banks.
+    const char* pbase = (const char*)((AXIS == 0 ? X : dY) + (int64_t)first * p_ld);
+    const char* qbase = (const char*)((AXIS == 0 ? dY : X) + (int64_t)first * q_ld);
+    uint32_t pcol[2], qcol[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int c = (lane & 31) ^ ((q * 2 + (lane >> 5)) << 2);
+        pcol[q] = (uint32_t)min(p0 + c * 8, (dP - 1) / 8 * 8) * 2u;
+        qcol[q] = (uint32_t)min(q0 + c * 8, (dQ - 1) / 8 * 8) * 2u;
+    }
+    const int tok = wave * 8 + (lane >> 5), n = end - first;
+    auto request = [&](int s, uint32_t stage) {
+        const int most = n - 1 - s * kGradTokens;     // rows behind the expert's last repeat it
+        const char* pb = pbase + (int64_t)s * kGradTokens * p_ld * 2;
+        const char* qb = qbase + (int64_t)s * kGradTokens * q_ld * 2;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t row = (uint32_t)min(tok + q * 2, most);
+            load_lds_16(lds0 + stage + (wave * 4 + q) * 1024, row * (uint32_t)p_ld * 2u + pcol[q & 1], pb);
+            load_lds_16(lds0 + stage + kGradOperand + (wave * 4 + q) * 1024, row * (uint32_t)q_ld * 2u + qcol[q & 1], qb);
         }
     };
-    float16v acc;
+    // (what the wave has loaded itself: nothing but its own loads has to be waited for)
+    auto clear_behind = [&](int s, uint32_t stage) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-    for (int m0 = first; m0 < end; m0 += kGradTokens) {
-        stage(P, dP, p0, m0, Ps);
-        stage(Q, dQ, q0, m0, Qs);
-        __syncthreads();
-        const int at = (lane & 31) * kGradLD + (lane >> 5) * 8;
+        for (int q = 0; q < 4; ++q)
+            if (s * kGradTokens + tok + q * 2 >= n) {
+                *(uint4v*)(grad_smem + stage + (wave * 4 + q) * 1024 + lane * 16) = (uint4v){0, 0, 0, 0};
+                *(uint4v*)(grad_smem + stage + kGradOperand + (wave * 4 + q) * 1024 + lane * 16) = (uint4v){0, 0, 0, 0};
+            }
+    };
+
+    float16v acc[FP][FQ];
 #pragma unroll
-        for (int ks = 0; ks < kGradTokens; ks += 16) {
-            const uint4v a = *(const uint4v*)(Ps + (wave >> 1) * 32 * kGradLD + at + ks);
-            const uint4v b = *(const uint4v*)(Qs + (wave & 1) * 32 * kGradLD + at + ks);
-            acc = mfma32<DT>(a, b, acc);
+    for (int f = 0; f < FP; ++f)
+#pragma unroll
+        for (int h = 0; h < FQ; ++h)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[f][h][r] = 0.f;
+
+    // this lane's part of a transposing read: token (lane / 32) * 8 + lane % 16 / 4, columns (lane / 16 % 2) * 16 + lane % 4 * 4; 32
+    // columns further is 64 bytes, exclusive or with the place's own bits
+    const int tr = (lane & 15) >> 2;
+    const uint32_t row_at = (uint32_t)((lane >> 5) * 8 + tr) * 512u, col_at = (uint32_t)(((lane >> 4) & 1) * 32 + (lane & 3) * 8);
+    uint32_t p_at[FP], q_at[FQ];
+#pragma unroll
+    for (int f = 0; f < FP; ++f) p_at[f] = row_at + ((uint32_t)(wp * 256 + f * 64 + col_at) ^ (uint32_t)(tr << 6));
+#pragma unroll
+    for (int h = 0; h < FQ; ++h) q_at[h] = kGradOperand + row_at + ((uint32_t)(wq * 128 + h * 64 + col_at) ^ (uint32_t)(tr << 6));
+    uint4v a[2][FP], b[2][FQ];
+    auto read_one = [&](uint32_t at) {
+        const uint2v lo = read_transposed(grad_smem + at), hi = read_transposed(grad_smem + at + 4 * 512);
+        return (uint4v){lo[0], lo[1], hi[0], hi[1]};
+    };
+    auto read_frags = [&](uint32_t stage, int ks) {
+#pragma unroll
+        for (int h = 0; h < FQ; ++h) b[ks & 1][h] = read_one(stage + ks * 16 * 512 + q_at[h]);
+#pragma unroll
+        for (int f = 0; f < FP; ++f) a[ks & 1][f] = read_one(stage + ks * 16 * 512 + p_at[f]);
+    };
+    auto multiply = [&](int ks) {
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+            for (int h = 0; h < FQ; ++h) acc[f][h] = mfma32<DT>(a[ks & 1][f], b[ks & 1][h], acc[f][h]);
+    };
+
+    const int n_steps = (n + kGradTokens - 1) / kGradTokens;
+    request(0, 0);
+    auto step = [&](int s, uint32_t cur, uint32_t nxt) {
+        wait_loads<0>();
+        if ((s + 1) * kGradTokens > n) clear_behind(s, cur);
+        lds_barrier();                                // step s is there, and nobody reads the other stage any more
+        if (s + 1 < n_steps) request(s + 1, nxt);
+        read_frags(cur, 0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks < 3) read_frags(cur, ks + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(ks);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __syncthreads();
+    };
+    for (int s = 0; s < n_steps; s += 2) {
+        step(s, 0, kGradStage);
+        if (s + 1 < n_steps) step(s + 1, kGradStage, 0);
     }
+
     // 32x32 accumulator: element r of lane l is row (r/4)*8 + (l/32)*4 + r%4, column l%32
-    const uint32_t* words = B_packed + (int64_t)e * d_out * (d_in / 32);
-    const int pw = p0 + (wave >> 1) * 32, q = q0 + (wave & 1) * 32 + (lane & 31);
-    const int qc = min(q, dQ - 1);
-    float sum = 0.f;
+    float sum[FQ] = {0.f, 0.f};
+    auto add = [&](int h, float x, uint32_t word, int left) {     // +-x by the bit that `left` brings to the top
+        const uint32_t one = ((word << left) & 0x80000000u) ^ 0xBF800000u;
+        sum[h] = __builtin_fmaf(x, __builtin_bit_cast(float, one), sum[h]);
+    };
+    __syncthreads();                                  // the stages are free
+    uint32_t* tile_signs = (uint32_t*)grad_smem;      // column mode: [256][8]
+    float* red = (float*)(grad_smem + 8192);          // [2][256]
+    if constexpr (AXIS == 0) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int row = (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
-        const int o = AXIS == 0 ? qc : min(pw + row, d_out - 1), i = AXIS == 0 ? min(pw, d_in - 32) + row : qc;
-        const uint32_t plus = (words[(int64_t)o * (d_in / 32) + i / 32] >> (i & 31)) & 1u;
-        sum += plus ? acc[r] : -acc[r];               // (rows behind the matrix are zero)
+        for (int f = 0; f < FP; ++f) {
+            if (p0 + wp * 128 + f * 32 >= dP) continue;           // uniform: d_in is a multiple of 32
+#pragma unroll
+            for (int h = 0; h < FQ; ++h) {
+                const uint32_t word = sw[h][f] >> ((lane >> 5) * 4);              // the lane's rows are bits 0-3, 8-11, 16-19, 24-27
+#pragma unroll
+                for (int r = 0; r < 16; ++r) add(h, acc[f][h][r], word, 31 - ((r >> 2) * 8 + (r & 3)));
+            }
+        }
+    } else {
+        *(uint4v*)(tile_signs + threadIdx.x * 4) = (uint4v){sw[0][0], sw[0][1], sw[0][2], sw[0][3]};
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = wp * 128 + f * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
+                const uint2v w = *(const uint2v*)(tile_signs + row * 8 + wq * 2);
+                const bool real = p0 + row < dP;
+#pragma unroll
+                for (int h = 0; h < FQ; ++h) {
+                    const uint32_t wh = w[h];
+                    add(h, real ? acc[f][h][r] : 0.f, wh, 31 - (lane & 31));
+                }
+            }
     }
-    sum += __shfl_xor(sum, 32, kWave);
-    if (lane < 32) red[wave >> 1][(wave & 1) * 32 + lane] = sum;
+#pragma unroll
+    for (int h = 0; h < FQ; ++h) {
+        sum[h] += __shfl_xor(sum[h], 32, kWave);
+        if (lane < 32) red[wp * kGradTile + wq * 64 + h * 32 + lane] = sum[h];
+    }
     __syncthreads();
-    if (tid < kGradTile && q0 + tid < dQ)
-        partial[((int64_t)e * sum_tiles + st) * dQ + q0 + tid] = red[0][tid] + red[1][tid];
+    const int q = threadIdx.x;
+    if (q < kGradTile && q0 + q < dQ) partial[((int64_t)e * sum_tiles + st) * dQ + q0 + q] = red[q] + red[kGradTile + q];
 }
 
 // The sums of the tiles of one expert, in their order.
@@ -100,11 +223,16 @@ experts_grad_sum_kernel(const float* __restrict__ partial, const int* __restrict
     grad[(int64_t)e * dQ + q] = sum;
 }
 
+// dY with rows that are no multiple of 16 bytes is copied into rows that are, behind the tiles' sums.
+static int64_t sums_bytes(int64_t E, int64_t kept, int64_t summed)
+{
+    return (E * ((summed + kGradTile - 1) / kGradTile) * kept * 4 + 15) / 16 * 16;
+}
+
 size_t experts_grad_v_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
 {
-    (void)M;
-    const int64_t kept = axis == 0 ? d_out : d_in, summed = axis == 0 ? d_in : d_out;
-    return (size_t)E * (size_t)((summed + kGradTile - 1) / kGradTile) * (size_t)kept * 4;
+    const int64_t rows = (d_out & 7) != 0 ? M * experts_padded(d_out) * 2 : 0;
+    return (size_t)(sums_bytes(E, axis == 0 ? d_out : d_in, axis == 0 ? d_in : d_out) + rows);
 }
 
 template <int DT, int AXIS>
@@ -115,10 +243,21 @@ static int launch_grad(const void* X, const void* dY, const int* offsets, const 
     const int64_t kept_tiles = (kept + kGradTile - 1) / kGradTile, sum_tiles = (summed + kGradTile - 1) / kGradTile;
     const int64_t sum_blocks = (kept + 255) / 256;
     if (E * kept_tiles * sum_tiles > 0x7FFFFFFF || E * sum_blocks > 0x7FFFFFFF) return -2;
-    if (M > 0)
-        hipLaunchKernelGGL((experts_grad_kernel<DT, AXIS>), dim3((unsigned)(E * kept_tiles * sum_tiles)), dim3(256), 0, stream,
-                           (const uint16_t*)X, (const uint16_t*)dY, offsets, B_packed, (float*)workspace, (int)M, (int)d_out, (int)d_in,
+    auto kernel = experts_grad_kernel<DT, AXIS>;
+    static unsigned lds_opted_in = 0;                 // per template instance: one kernel
+    if (opt_in_dynamic_lds((const void*)kernel, kGradLds, &lds_opted_in) != 0) return -1;
+    int64_t y_ld = d_out;
+    if (M > 0) {
+        if ((d_out & 7) != 0) {
+            void* rows = (char*)workspace + sums_bytes(E, kept, summed);
+            y_ld = experts_padded(d_out);
+            launch_experts_copy_rows(dY, rows, M, d_out, stream);
+            dY = rows;
+        }
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(E * kept_tiles * sum_tiles)), dim3(512), kGradLds, stream, (const uint16_t*)X, (int)d_in,
+                           (const uint16_t*)dY, (int)y_ld, offsets, B_packed, (float*)workspace, (int)M, (int)d_out, (int)d_in,
                            (int)kept_tiles, (int)sum_tiles);
+    }
     hipLaunchKernelGGL(experts_grad_sum_kernel, dim3((unsigned)(E * sum_blocks)), dim3(256), 0, stream, (const float*)workspace, offsets,
                        grad, (int)M, (int)kept, (int)sum_tiles, (int)sum_blocks);
     return hipGetLastError() == hipSuccess ? 0 : -1;

@@ -154,6 +154,10 @@ size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64
 int launch_experts_linear(const ExpertsCall& c, hipStream_t stream);
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream);
 
+// Rows of K 16-bit values copied into rows of experts_padded(K), zeros behind them.
+constexpr int64_t experts_padded(int64_t K) { return (K + 127) / 128 * 128; }
+void launch_experts_copy_rows(const void* rows, void* out, int64_t M, int64_t K, hipStream_t stream);
+
 // Gradient with respect to every expert's scales.
 size_t experts_grad_v_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis);
 int launch_experts_grad_v(int dtype, int axis, const void* X, const void* dY, const int* offsets, const uint32_t* B_packed, float* grad,
