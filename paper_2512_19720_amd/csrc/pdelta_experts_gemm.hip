@@ -172,7 +172,7 @@ void launch_experts_copy_rows(const void* rows, void* out, int64_t M, int64_t K,
 }
 
 // The prepared token operand: fp16 rows of `lda` values, behind them an fp32 factor for each row.
-static bool needs_prepare(int64_t K, int dtype) { return dtype == kBF16 || (K & 7) != 0; }
+static bool needs_prepare(int64_t K, int dtype) { return dtype == kBF16 || (K & 127) != 0; }
 
 static size_t prepared_bytes(int64_t M, int64_t K, int dtype)
 {
@@ -211,6 +211,8 @@ static int launch_product(const ExpertsCall& c, bool grad, hipStream_t stream)
         }
         A = rows;
     }
+    const int bm = tune_value("experts_bm", c.M / c.E >= 192 ? 256 : 128);
+    if ((grad || (K & 127) == 0) && bm >= 128) return launch_experts_big(c, grad, bm, A, lda, inverse, stream);
 #define PDELTA_GO(WDT, AXIS) \
     return grad ? launch_tiles<WDT, AXIS, true>(c, A, lda, inverse, stream) : launch_tiles<WDT, AXIS, false>(c, A, lda, inverse, stream)
     if (c.dtype == kBF16) {

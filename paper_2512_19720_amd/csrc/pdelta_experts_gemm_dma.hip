@@ -1,0 +1,299 @@
+// Products of tokens sorted by expert with W_hat (forward) or its transpose (GRAD) on tiles of BM tokens x 256 outputs x 64 of
+// the contraction, 8 waves of BM / 2 x 64 outputs, all global traffic as direct loads into LDS.  The arithmetic is that of
+// pdelta_experts_gemm.hip, and the schedule that of the dense 256 x 256 prefill kernel: two LDS stages; a wave turns the pieces of
+// W_b that it has itself loaded into W_hat in place, between its matrix instructions; one barrier per step, three quarters into
+// it, which publishes step s + 1 and frees the stage of step s for step s + 2.
+//
+// The tokens come as fp16 rows of a multiple of 128 values (prepared ones, or X and dY themselves).
+//
+// Forward: a tile of W_hat is 256 output rows x 64 inputs; both operands' fragments are 16 consecutive bytes of a row.
+// GRAD: it is 64 output rows x 256 inputs, as it lies in memory, and the contraction runs over the rows: fragments are read by
+// transposing LDS reads, 4 rows x 16 columns for 16 lanes.  Nothing is transposed in memory, and the signs and scales are those of
+// the forward layout.
+//
+// Workgroup -> tile: the XCD w % 8 takes a contiguous range of the tiles, which are numbered expert by expert, then by output
+// tile, then by token tile, so that the CUs of an XCD share panels of W_b in its L2.
+#include <algorithm>
+#include <type_traits>
+
+#include "pdelta_experts.h"
+#include "pdelta_gemm_tile.h"
+#include "pdelta_host.h"
+#include "pdelta_lds_load.h"
+
+namespace pdelta {
+
+constexpr int kTileN = 256, kTileK = 64;
+constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
+// behind the stages: a wave's signs (1 KB: forward, its 32 rows for four steps; GRAD, its 8 rows of 256 inputs), and its scales (1 KB:
+// forward column mode, four steps' v; GRAD row mode, its 8 rows')
+constexpr int tile_lds(int bm) { return 2 * (bm * kTileK * 2 + kWBytes) + 8 * 2048; }
+
+template <int WDT, int AXIS, bool GRAD, int BM>
+__global__ void __launch_bounds__(512, 2)
+experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
+                   const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
+                   const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out, int d_in, int y_dtype, int n_tiles)
+{
+    constexpr int FM = BM / 64, FN = 2, AQ = BM / 64; // MFMA tiles of a wave; load instructions of a wave for the tokens of a step
+    constexpr int AB = BM * kTileK * 2, STAGE = AB + kWBytes, SIGNS = 2 * STAGE, SCALES = SIGNS + 8 * 1024;
+    extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
+
+    ExpertTile t;
+    int tile_n;
+    if (!find_expert_block<BM>(offsets, E, M, n_tiles, (int)blockIdx.x % kXcds, (int)blockIdx.x / kXcds, t, tile_n)) return;  // whole workgroup
+    const int N = GRAD ? d_in : d_out;
+    const int n0 = tile_n * kTileN, n_steps = lda / kTileK;       // even, at least 2
+    const uint16_t* W = W_b + t.expert * w_stride;
+    const uint32_t* B = B_packed + (int64_t)t.expert * d_out * (d_in / 32);
+    const uint16_t* scales = v + (int64_t)t.expert * (AXIS == 0 ? d_out : d_in);
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave >> 2, wn = wave & 3;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)tile_smem;
+
+    // Tokens: a load instruction covers 8 rows of 128 bytes; the 16-byte piece p of row r holds values 8 (p ^ ((r >> 1) & 7)) .. +7.
+    // Rows behind the expert's last one repeat it (they feed outputs that are never stored).
+    const char* abase = (const char*)(A + (int64_t)t.row0 * lda);
+    uint32_t aoff[AQ], piece[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) piece[q] = (uint32_t)((lane & 7) ^ (q * 4 + (lane >> 4)));
+#pragma unroll
+    for (int q = 0; q < AQ; ++q)
+        aoff[q] = (uint32_t)(min(t.row0 + wave * (BM / 8) + q * 8 + (lane >> 3), t.end - 1) - t.row0) * (uint32_t)lda * 2u + piece[q & 1] * 16u;
+
+    // W_b.  Forward: the same for the tile's 256 output rows.  GRAD: a load instruction covers 512 bytes of two rows; the piece c of
+    // row r is at place c ^ 4 (r & 3), which puts the four rows of a transposing read into different banks.
+    const char* wbase;
+    const char* sbase;
+    uint32_t woff[4], soff, chunk[2];
+    uint32_t vrow[4];                                 // forward row mode: the scale of the wave's rows
+    uint4v vcol[2];                                   // GRAD column mode: the scales of the lane's inputs
+    if constexpr (GRAD) {
+        wbase = (const char*)W;
+        sbase = (const char*)B;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            chunk[q] = (uint32_t)((lane & 31) ^ ((q * 2 + (lane >> 5)) << 2));
+            const int col = min(n0 + (int)chunk[q] * 8, d_in - 8);
+            woff[q] = (uint32_t)col * 2u;
+            if constexpr (AXIS == 1) vcol[q] = *(const uint4v*)(scales + col);
+        }
+        soff = (uint32_t)min(n0 / 32 + (lane & 7), d_in / 32 - 1) * 4u;
+    } else {
+        wbase = (const char*)(W + (int64_t)n0 * d_in);
+        sbase = (const char*)B + (int64_t)n0 * (d_in >> 3);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) chunk[q] = piece[q];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int row = min(n0 + wave * 32 + q * 8 + (lane >> 3), d_out - 1) - n0;
+            woff[q] = (uint32_t)row * (uint32_t)d_in * 2u + chunk[q & 1] * 16u;
+            if constexpr (AXIS == 0) vrow[q] = (uint32_t)scales[n0 + row] * 0x10001u;
+        }
+        // lanes 0-31: sign words of the wave's rows for two steps, lanes 32-63 for the next two
+        soff = (uint32_t)(min(n0 + wave * 32 + (lane & 31), d_out - 1) - n0) * (uint32_t)(d_in >> 3) + (lane >> 5) * 16u;
+    }
+
+    auto request = [&](int s, uint32_t stage) {
+        const int kb = s * kTileK;
+        if constexpr (GRAD) {
+            // rows behind the last one repeat it: the tokens are zero there
+            const int k0 = min(kb, d_out - 1);
+            auto row = [&](int r) { return (uint32_t)(min(kb + r, d_out - 1) - k0); };
+            load_lds_4(lds0 + SIGNS + wave * 1024, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
+            if constexpr (AXIS == 0)
+                if (lane < 8) load_lds_2(lds0 + SCALES + wave * 1024, row(wave * 8 + lane) * 2u, scales + k0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                load_lds_16(lds0 + stage + AB + (wave * 4 + q) * 1024, row(wave * 8 + q * 2 + (lane >> 5)) * (uint32_t)d_in * 2u + woff[q & 1],
+                            wbase + (int64_t)k0 * d_in * 2);
+        } else {
+            if ((s & 3) == 0) {                       // never past d_in: a short last group repeats its first half
+                load_lds_16(lds0 + SIGNS + wave * 1024, kb + 128 < d_in ? soff : soff - (lane >> 5) * 16u, sbase + (kb >> 3));
+                if constexpr (AXIS == 1)
+                    load_lds_16(lds0 + SCALES + wave * 1024, (uint32_t)min(kb + (lane & 31) * 8, d_in - 8) * 2u, scales);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) load_lds_16(lds0 + stage + AB + (wave * 4 + q) * 1024, woff[q], wbase + (int64_t)kb * 2);
+        }
+#pragma unroll
+        for (int q = 0; q < AQ; ++q) load_lds_16(lds0 + stage + (wave * AQ + q) * 1024, aoff[q], abase + (int64_t)kb * 2);
+    };
+
+    // In place: the wave's own pieces of W_b -> W_hat.
+    uint4v raw[4], wvec[2];
+    uint32_t sbyte[4], wscale[4];
+    auto fetch_w = [&](int s, uint32_t stage) {
+        const unsigned char* sg = tile_smem + SIGNS + wave * 1024;
+        const unsigned char* sc = tile_smem + SCALES + wave * 1024;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            raw[q] = *(const uint4v*)(tile_smem + stage + AB + (wave * 4 + q) * 1024 + lane * 16);
+            if constexpr (GRAD) {
+                sbyte[q] = sg[(q * 2 + (lane >> 5)) * 32 + chunk[q & 1]];
+                if constexpr (AXIS == 0) wscale[q] = *(const uint16_t*)(sc + (q * 2 + (lane >> 5)) * 4);
+            } else {
+                sbyte[q] = sg[((s >> 1) & 1) * 512 + (s & 1) * 8 + (q * 8 + (lane >> 3)) * 16 + chunk[q & 1]];
+            }
+        }
+        if constexpr (!GRAD && AXIS == 1) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) wvec[q] = *(const uint4v*)(sc + (s & 3) * 128 + chunk[q] * 16);
+        }
+    };
+    auto convert_w = [&](uint32_t stage) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t minus = ~sbyte[q] & 0xFFu;
+            uint32_t y = minus | (minus << 15);       // bit 2p + 1 at 2p + 16
+            asm("" : "+v"(y));                        // (else y and its shifts become full multiplications)
+            uint32_t vv = 0;
+            if constexpr (AXIS == 0) vv = GRAD ? wscale[q] | (wscale[q] << 16) : vrow[q];
+            const uint4v w16 = to_f16x8<WDT>(raw[q]);
+            uint4v r;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                uint32_t vp = vv;
+                if constexpr (AXIS == 1) vp = GRAD ? vcol[q & 1][p] : wvec[q & 1][p];
+                const uint32_t wp = w16[p], sv = ((y << (15 - 2 * p)) & 0x80008000u) ^ vp;      // -v where the bit is set
+                r[p] = as_u32(as_half2(wp) + as_half2(sv));
+            }
+            *(uint4v*)(tile_smem + stage + AB + (wave * 4 + q) * 1024 + lane * 16) = r;
+        }
+    };
+
+    float16v acc[FM][FN];
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int h = 0; h < FN; ++h)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[f][h][r] = 0.f;
+
+    // this lane's piece of 16 values ks of a row is at byte frag ^ (32 ks)
+    const uint32_t frag = (uint32_t)((lane & 31) * 128 + (((lane >> 5) ^ ((lane >> 1) & 7)) * 16));
+    // GRAD: row (lane / 32) * 8 + lane % 16 / 4, columns (lane / 16 % 2) * 16 + lane % 4 * 4; 32 columns further: exclusive or 64
+    const int tr = (lane & 15) >> 2;
+    const uint32_t tfrag = (uint32_t)((lane >> 5) * 8 + tr) * 512u +
+                           ((uint32_t)(wn * 128 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8) ^ (uint32_t)(tr << 6));
+    half8 a[2][FM], b[2][FN];
+    auto read_frags = [&](uint32_t stage, auto step16) {
+        constexpr int ks = decltype(step16)::value;
+        const uint32_t at = frag ^ (uint32_t)(ks * 32);
+        const unsigned char* xa = tile_smem + stage + wm * (BM / 2) * 128 + at;
+#pragma unroll
+        for (int h = 0; h < FN; ++h) {
+            if constexpr (GRAD) {
+                const unsigned char* p = tile_smem + stage + AB + ks * 16 * 512 + (tfrag ^ (uint32_t)(h * 64));
+                const uint2v lo = read_transposed(p), hi = read_transposed(p + 4 * 512);
+                b[ks & 1][h] = __builtin_bit_cast(half8, (uint4v){lo[0], lo[1], hi[0], hi[1]});
+            } else {
+                b[ks & 1][h] = *(const half8*)(tile_smem + stage + AB + wn * 64 * 128 + at + h * 32 * 128);
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < FM; ++f) a[ks & 1][f] = *(const half8*)(xa + f * 32 * 128);
+    };
+    auto multiply = [&](int ks) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int h = 0; h < FN; ++h)
+                acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks & 1][f], b[ks & 1][h], acc[f][h], 0, 0, 0);
+    };
+
+    request(0, 0);
+    wait_loads<0>();
+    fetch_w(0, 0);
+    convert_w(0);
+    lds_barrier();
+    request(1, STAGE);
+    read_frags(0, std::integral_constant<int, 0>{});
+
+    // Step s; REQ: request step s + 2, MORE: there is a step s + 1.  The fences keep the LDS reads above the MFMAs and the
+    // conversion between them.
+    auto step = [&](int s, uint32_t cur, uint32_t nxt, auto req, auto more) {
+        constexpr bool REQ = decltype(req)::value, MORE = decltype(more)::value;
+        constexpr int VALU = (WDT == kBF16 ? 13 : 7) * 8 / (FM * FN);     // vector instructions after each MFMA of a quarter
+        read_frags(cur, std::integral_constant<int, 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (MORE) wait_loads<AQ>();         // (the last ones are the tokens')
+        if constexpr (MORE) fetch_w(s + 1, nxt);
+        read_frags(cur, std::integral_constant<int, 2>{});
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1);
+        if constexpr (MORE) { convert_w(nxt); interleave<FM * FN, VALU>(); }
+        __builtin_amdgcn_sched_barrier(0);
+        read_frags(cur, std::integral_constant<int, 3>{});
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(2);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (MORE) wait_loads<0>();
+        lds_barrier();
+        if constexpr (MORE) read_frags(nxt, std::integral_constant<int, 0>{});
+        if constexpr (REQ) request(s + 2, cur);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(3);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int s = 0;
+    for (; s + 2 < n_steps; s += 2) {
+        step(s, 0, STAGE, std::true_type{}, std::true_type{});
+        step(s + 1, STAGE, 0, std::true_type{}, std::true_type{});
+    }
+    step(s, 0, STAGE, std::false_type{}, std::true_type{});
+    step(s + 1, STAGE, 0, std::false_type{}, std::false_type{});
+
+    // (the last barrier came after the last fragment read: the stages are free)
+    const int m0 = t.row0 + wm * (BM / 2);
+    if (inverse != nullptr) {
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float x = inverse[min(m0 + f * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3), t.end - 1)];
+#pragma unroll
+                for (int h = 0; h < FN; ++h) acc[f][h][r] *= x;
+            }
+    }
+    store_wave_tile<FM>(acc, (uint16_t*)tile_smem + wave * 32 * kGemmLDK, Y, y_dtype, m0, n0 + wn * 64, t.end, N, lane);
+}
+
+template <int WDT, int AXIS, bool GRAD, int BM>
+static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
+{
+    constexpr int lds = tile_lds(BM);
+    const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
+    const int64_t blocks = (most_expert_tiles(c.M, c.E, BM) * n_tiles + kXcds - 1) / kXcds * kXcds;
+    if (blocks > 0x7FFFFFFF) return -2;
+    auto kernel = experts_big_kernel<WDT, AXIS, GRAD, BM>;
+    static unsigned lds_opted_in = 0;                 // per template instance: one kernel
+    if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), lds, stream, A, lda, inverse, c.offsets, (const uint16_t*)c.W_b, c.w_stride,
+                       c.B_packed, c.v, c.out, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+int launch_experts_big(const ExpertsCall& c, bool grad, int bm, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
+{
+#define PDELTA_GO(WDT, AXIS, GRAD)                                                                        \
+    return bm == 256 ? launch_big_tiles<WDT, AXIS, GRAD, 256>(c, A, lda, inverse, stream)               \
+                     : launch_big_tiles<WDT, AXIS, GRAD, 128>(c, A, lda, inverse, stream)
+    if (c.dtype == kBF16) {
+        if (c.axis == 0 && grad) PDELTA_GO(kBF16, 0, true);
+        if (c.axis == 0) PDELTA_GO(kBF16, 0, false);
+        if (grad) PDELTA_GO(kBF16, 1, true);
+        PDELTA_GO(kBF16, 1, false);
+    }
+    if (c.axis == 0 && grad) PDELTA_GO(kF16, 0, true);
+    if (c.axis == 0) PDELTA_GO(kF16, 0, false);
+    if (grad) PDELTA_GO(kF16, 1, true);
+    PDELTA_GO(kF16, 1, false);
+#undef PDELTA_GO
+}
+
+}  // namespace pdelta

@@ -28,14 +28,6 @@ __device__ __forceinline__ float16v mfma32(uint4v a, uint4v b, float16v c)
 constexpr int kGradTile = 256, kGradTokens = 64;
 constexpr int kGradOperand = kGradTokens * kGradTile * 2, kGradStage = 2 * kGradOperand, kGradLds = 2 * kGradStage;
 
-typedef short short4v __attribute__((ext_vector_type(4)));
-// Four values of one column from 16 lanes' rows of four: lane 4 r + c of 16 points at columns 4 c .. 4 c + 3 of row r, lane i gets
-// rows 0 .. 3 of column i.
-__device__ __forceinline__ uint2v read_transposed(const unsigned char* p)
-{
-    return __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)p));
-}
-
 template <int DT, int AXIS>
 __global__ void __launch_bounds__(512, 2)
 experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __restrict__ dY, int y_ld, const int* __restrict__ offsets,
