@@ -211,8 +211,7 @@ static int launch_product(const ExpertsCall& c, bool grad, hipStream_t stream)
         }
         A = rows;
     }
-    const int bm = tune_value("experts_bm", c.M / c.E >= 192 ? 256 : 128);
-    if ((grad || (K & 127) == 0) && bm >= 128) return launch_experts_big(c, grad, bm, A, lda, inverse, stream);
+    if (grad || (K & 127) == 0) return launch_experts_big(c, grad, A, lda, inverse, stream);
 #define PDELTA_GO(WDT, AXIS) \
     return grad ? launch_tiles<WDT, AXIS, true>(c, A, lda, inverse, stream) : launch_tiles<WDT, AXIS, false>(c, A, lda, inverse, stream)
     if (c.dtype == kBF16) {

@@ -1,5 +1,5 @@
-// Products of tokens sorted by expert with W_hat (forward) or its transpose (GRAD) on tiles of BM tokens x 256 outputs x 64 of
-// the contraction, 8 waves of BM / 2 x 64 outputs, all global traffic as direct loads into LDS.  The arithmetic is that of
+// Products of tokens sorted by expert with W_hat (forward) or its transpose (GRAD) on tiles of up to 256 tokens x 256 outputs x 64
+// of the contraction, 8 waves, all global traffic as direct loads into LDS.  The arithmetic is that of
 // pdelta_experts_gemm.hip, and the schedule that of the dense 256 x 256 prefill kernel: two LDS stages; a wave turns the pieces of
 // W_b that it has itself loaded into W_hat in place, between its matrix instructions; one barrier per step, three quarters into
 // it, which publishes step s + 1 and frees the stage of step s for step s + 2.
@@ -23,29 +23,38 @@
 
 namespace pdelta {
 
-constexpr int kTileN = 256, kTileK = 64;
+constexpr int kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
 // behind the stages: a wave's signs (1 KB: forward, its 32 rows for four steps; GRAD, its 8 rows of 256 inputs), and its scales (1 KB:
 // forward column mode, four steps' v; GRAD row mode, its 8 rows')
-constexpr int tile_lds(int bm) { return 2 * (bm * kTileK * 2 + kWBytes) + 8 * 2048; }
+constexpr int kTileLds = 2 * (kTileM * kTileK * 2 + kWBytes) + 8 * 2048;
 
-template <int WDT, int AXIS, bool GRAD, int BM>
-__global__ void __launch_bounds__(512, 2)
-experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
-                   const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
-                   const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out, int d_in, int y_dtype, int n_tiles)
+struct TileArgs {
+    const uint16_t* A;
+    int lda;
+    const float* inverse;
+    const uint16_t* W_b;
+    int64_t w_stride;
+    const uint32_t* B_packed;
+    const uint16_t* v;
+    void* Y;
+    int d_out, d_in, y_dtype;
+};
+
+// One tile of 64 FM tokens, waves of 32 FM x 64 outputs.
+template <int WDT, int AXIS, bool GRAD, int FM>
+__device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile& t, int tile_n, unsigned char* tile_smem)
 {
-    constexpr int FM = BM / 64, FN = 2, AQ = BM / 64; // MFMA tiles of a wave; load instructions of a wave for the tokens of a step
+    constexpr int BM = FM * 64, FN = 2, AQ = FM;      // tokens; MFMA tiles of a wave along outputs; load instructions of a wave for the tokens
     constexpr int AB = BM * kTileK * 2, STAGE = AB + kWBytes, SIGNS = 2 * STAGE, SCALES = SIGNS + 8 * 1024;
-    extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
-
-    ExpertTile t;
-    int tile_n;
-    if (!find_expert_block<BM>(offsets, E, M, n_tiles, (int)blockIdx.x % kXcds, (int)blockIdx.x / kXcds, t, tile_n)) return;  // whole workgroup
+    const uint16_t *A = g.A, *v = g.v;
+    const float* inverse = g.inverse;
+    const int lda = g.lda, d_out = g.d_out, d_in = g.d_in, y_dtype = g.y_dtype;
+    void* Y = g.Y;
     const int N = GRAD ? d_in : d_out;
     const int n0 = tile_n * kTileN, n_steps = lda / kTileK;       // even, at least 2
-    const uint16_t* W = W_b + t.expert * w_stride;
-    const uint32_t* B = B_packed + (int64_t)t.expert * d_out * (d_in / 32);
+    const uint16_t* W = g.W_b + t.expert * g.w_stride;
+    const uint32_t* B = g.B_packed + (int64_t)t.expert * d_out * (d_in / 32);
     const uint16_t* scales = v + (int64_t)t.expert * (AXIS == 0 ? d_out : d_in);
 
     const int lane = threadIdx.x & 63;
@@ -61,7 +70,8 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
     for (int q = 0; q < 2; ++q) piece[q] = (uint32_t)((lane & 7) ^ (q * 4 + (lane >> 4)));
 #pragma unroll
     for (int q = 0; q < AQ; ++q)
-        aoff[q] = (uint32_t)(min(t.row0 + wave * (BM / 8) + q * 8 + (lane >> 3), t.end - 1) - t.row0) * (uint32_t)lda * 2u + piece[q & 1] * 16u;
+        aoff[q] = (uint32_t)(min(t.row0 + wave * (BM / 8) + q * 8 + (lane >> 3), t.end - 1) - t.row0) * (uint32_t)lda * 2u +
+                  (uint32_t)((lane & 7) ^ (((wave * FM + q) & 1) * 4 + (lane >> 4))) * 16u;
 
     // W_b.  Forward: the same for the tile's 256 output rows.  GRAD: a load instruction covers 512 bytes of two rows; the piece c of
     // row r is at place c ^ 4 (r & 3), which puts the four rows of a transposing read into different banks.
@@ -216,7 +226,7 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
     // conversion between them.
     auto step = [&](int s, uint32_t cur, uint32_t nxt, auto req, auto more) {
         constexpr bool REQ = decltype(req)::value, MORE = decltype(more)::value;
-        constexpr int VALU = (WDT == kBF16 ? 13 : 7) * 8 / (FM * FN);     // vector instructions after each MFMA of a quarter
+        constexpr int VALU = ((WDT == kBF16 ? 13 : 7) * 8 + FM * FN - 1) / (FM * FN);     // vector instructions after each MFMA of a quarter
         read_frags(cur, std::integral_constant<int, 1>{});
         __builtin_amdgcn_sched_barrier(0);
         multiply(0);
@@ -263,14 +273,33 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
     store_wave_tile<FM>(acc, (uint16_t*)tile_smem + wave * 32 * kGemmLDK, Y, y_dtype, m0, n0 + wn * 64, t.end, N, lane);
 }
 
-template <int WDT, int AXIS, bool GRAD, int BM>
+// A tile of fewer tokens takes as many MFMA tiles as they need: the ends of ragged experts cost what they are.
+template <int WDT, int AXIS, bool GRAD>
+__global__ void __launch_bounds__(512, 2)
+experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
+                   const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
+                   const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out, int d_in, int y_dtype, int n_tiles)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
+    ExpertTile t;
+    int tile_n;
+    if (!find_expert_block<kTileM>(offsets, E, M, n_tiles, (int)blockIdx.x % kXcds, (int)blockIdx.x / kXcds, t, tile_n)) return;  // whole workgroup
+    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, d_out, d_in, y_dtype};
+    const int rows = t.end - t.row0;
+    if (rows > 192) experts_tile<WDT, AXIS, GRAD, 4>(g, t, tile_n, tile_smem);
+    else if (rows > 128) experts_tile<WDT, AXIS, GRAD, 3>(g, t, tile_n, tile_smem);
+    else if (rows > 64) experts_tile<WDT, AXIS, GRAD, 2>(g, t, tile_n, tile_smem);
+    else experts_tile<WDT, AXIS, GRAD, 1>(g, t, tile_n, tile_smem);
+}
+
+template <int WDT, int AXIS, bool GRAD>
 static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
 {
-    constexpr int lds = tile_lds(BM);
+    constexpr int lds = kTileLds;
     const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
-    const int64_t blocks = (most_expert_tiles(c.M, c.E, BM) * n_tiles + kXcds - 1) / kXcds * kXcds;
+    const int64_t blocks = (most_expert_tiles(c.M, c.E, kTileM) * n_tiles + kXcds - 1) / kXcds * kXcds;
     if (blocks > 0x7FFFFFFF) return -2;
-    auto kernel = experts_big_kernel<WDT, AXIS, GRAD, BM>;
+    auto kernel = experts_big_kernel<WDT, AXIS, GRAD>;
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), lds, stream, A, lda, inverse, c.offsets, (const uint16_t*)c.W_b, c.w_stride,
@@ -278,11 +307,9 @@ static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, co
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_experts_big(const ExpertsCall& c, bool grad, int bm, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
+int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
 {
-#define PDELTA_GO(WDT, AXIS, GRAD)                                                                        \
-    return bm == 256 ? launch_big_tiles<WDT, AXIS, GRAD, 256>(c, A, lda, inverse, stream)               \
-                     : launch_big_tiles<WDT, AXIS, GRAD, 128>(c, A, lda, inverse, stream)
+#define PDELTA_GO(WDT, AXIS, GRAD) return launch_big_tiles<WDT, AXIS, GRAD>(c, A, lda, inverse, stream)
     if (c.dtype == kBF16) {
         if (c.axis == 0 && grad) PDELTA_GO(kBF16, 0, true);
         if (c.axis == 0) PDELTA_GO(kBF16, 0, false);

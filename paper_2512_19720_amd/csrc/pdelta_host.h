@@ -154,9 +154,9 @@ size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64
 int launch_experts_linear(const ExpertsCall& c, hipStream_t stream);
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream);
 
-// The same on tiles of 256 outputs with direct loads, bm (128 or 256) tokens: A holds fp16 rows of lda values, a multiple of 128;
+// The same on tiles of 256 outputs with direct loads: A holds fp16 rows of lda values, a multiple of 128;
 // inverse: a factor for each row of the outputs, or NULL.  Forward: d_in a multiple of 128.
-int launch_experts_big(const ExpertsCall& c, bool grad, int bm, const uint16_t* A, int lda, const float* inverse, hipStream_t stream);
+int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, hipStream_t stream);
 
 // Rows of K 16-bit values copied into rows of experts_padded(K), zeros behind them.
 constexpr int64_t experts_padded(int64_t K) { return (K + 127) / 128 * 128; }
