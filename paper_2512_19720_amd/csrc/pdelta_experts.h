@@ -2,12 +2,15 @@
 // offsets[e] .. offsets[e + 1] - 1 of the token matrices.
 #pragma once
 
+#include <algorithm>
+
 #include "pdelta_device.h"
 
 namespace pdelta {
 
-// Rows of one tile of up to BM tokens of one expert; `end` is the first row behind the expert's own.
-struct ExpertTile { int expert, row0, end; };
+// Rows of one tile of up to BM tokens of one expert; `end` is the first row behind the expert's own.  It is the `index`-th of
+// the expert's `tiles`.
+struct ExpertTile { int expert, row0, end, index, tiles; };
 
 // The tokens of expert e, in bounds whatever the offsets hold; without offsets all of them (one expert).
 __device__ __forceinline__ void expert_rows(const int* __restrict__ offsets, int e, int M, int& first, int& end)
@@ -41,7 +44,9 @@ __device__ __forceinline__ bool find_expert_tile(const int* __restrict__ offsets
         if (tile < all) {
             const int at = __builtin_ctzll(__ballot(upto > tile));
             out.expert = e0 + at;
-            out.row0 = __builtin_amdgcn_readlane(first, at) + (tile - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at))) * BM;
+            out.tiles = __builtin_amdgcn_readlane(tiles, at);
+            out.index = tile - (__builtin_amdgcn_readlane(upto, at) - out.tiles);
+            out.row0 = __builtin_amdgcn_readlane(first, at) + out.index * BM;
             out.end = __builtin_amdgcn_readlane(end, at);
             return true;
         }
@@ -50,55 +55,105 @@ __device__ __forceinline__ bool find_expert_tile(const int* __restrict__ offsets
     return false;
 }
 
-// The tile of output tile and token tile that a workgroup takes: XCD `xcd` takes a contiguous range of all tiles (numbered expert
-// by expert, then by output tile, then by token tile), the workgroup its `local`-th.  False (all lanes) behind the last.
+// The tiles of a product, up to BM tokens x one output tile each, numbered expert by expert, then by output tile, then by token
+// tile (an expert's last token tile may be a short one), dealt to the 8 XCDs in contiguous ranges of about the same cost: the CUs
+// of an XCD then share panels of weights in its L2.  A tile of 64 f tokens costs f + 2, as measured next to a full one.
 template <int BM>
-__device__ __forceinline__ bool find_expert_block(const int* __restrict__ offsets, int E, int M, int n_tiles, int xcd, int local,
-                                                  ExpertTile& out, int& tile_n)
-{
-    const int lane = threadIdx.x & 63;
-    int64_t tile = -1, all = 0, before = 0;           // first round: how many there are; second: where this one is
-    for (int round = 0; round < 2; ++round) {
-        before = 0;
-        for (int e0 = 0; e0 < E; e0 += kWave) {
-            int first, end;
-            expert_rows(offsets, min(e0 + lane, E - 1), M, first, end);
-            const int tiles = e0 + lane < E ? (end - first + BM - 1) / BM : 0;
-            int upto = tiles;
+struct ExpertTiles {
+    static constexpr int FULL = BM / 64 + 2;
+    const int* offsets;
+    int E, M, n_tiles;
+    int at, e0;                                       // this range's next tile; first expert of the chunk that the lanes hold
+    int first, end, tiles, cost;                      // of expert e0 + lane
+    int tiles_upto, cost_upto;                        // sums up to and with it
+    int tiles_before, cost_before;                    // sums of the chunks before
+
+    __device__ __forceinline__ int lane() const { return threadIdx.x & 63; }
+    __device__ __forceinline__ static int prefix(int x)
+    {
 #pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const int below = __shfl_up(upto, d, kWave);
-                if (lane >= d) upto += below;
-            }
-            const int here = __builtin_amdgcn_readlane(upto, kWave - 1);
-            if (round == 0 && E <= kWave) {           // one round is enough
-                all = (int64_t)here * n_tiles;
-                const int64_t per = (all + 7) / 8;
-                tile = xcd * per + local;
-                if (local >= per || tile >= all) return false;
-            }
-            if (tile >= 0 && tile < before + (int64_t)here * n_tiles) {
-                const int64_t rest = tile - before;
-                const int at = __builtin_ctzll(__ballot((int64_t)upto * n_tiles > rest));
-                const int mine = __builtin_amdgcn_readlane(tiles, at);
-                const int place = (int)(rest - (int64_t)(__builtin_amdgcn_readlane(upto, at) - mine) * n_tiles);
-                tile_n = place / mine;
-                out.expert = e0 + at;
-                out.row0 = __builtin_amdgcn_readlane(first, at) + place % mine * BM;
-                out.end = __builtin_amdgcn_readlane(end, at);
-                return true;
-            }
-            before += (int64_t)here * n_tiles;
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int below = __shfl_up(x, d, kWave);
+            if ((int)(threadIdx.x & 63) >= d) x += below;
         }
-        if (round == 0) {
-            all = before;
-            const int64_t per = (all + 7) / 8;
-            tile = xcd * per + local;
-            if (local >= per || tile >= all) return false;
+        return x;
+    }
+    __device__ __forceinline__ void chunk(int from, int tiles_sum, int cost_sum)
+    {
+        e0 = from;
+        tiles_before = tiles_sum;
+        cost_before = cost_sum;
+        expert_rows(offsets, min(e0 + lane(), E - 1), M, first, end);
+        if (e0 + lane() >= E) end = first;
+        const int rest = (end - first) % BM;
+        tiles = (end - first) / BM + (rest > 0);
+        cost = (end - first) / BM * FULL + (rest > 0 ? (rest + 63) / 64 + 2 : 0);
+        tiles_upto = prefix(tiles);
+        cost_upto = prefix(cost);
+    }
+    __device__ __forceinline__ int chunk_tiles() const { return __builtin_amdgcn_readlane(tiles_upto, kWave - 1); }
+    __device__ __forceinline__ int chunk_cost() const { return __builtin_amdgcn_readlane(cost_upto, kWave - 1); }
+    // Holds the chunk of the expert for which `found` (of the sums up to and with an expert) is true first; its lane, or -1.
+    template <typename F>
+    __device__ __forceinline__ int seek(F found)
+    {
+        if (E > kWave) chunk(0, 0, 0);                // (else the lanes hold all experts)
+        for (;;) {
+            const uint64_t hit = __ballot(found(tiles_before + tiles_upto, cost_before + cost_upto));
+            if (hit != 0) return __builtin_ctzll(hit);
+            if (e0 + kWave >= E) return -1;
+            chunk(e0 + kWave, tiles_before + chunk_tiles(), cost_before + chunk_cost());
         }
     }
-    return false;
-}
+    // Number of the first tile with at least `bound` of cost before it.
+    __device__ __forceinline__ int first_at(int bound, int all)
+    {
+        const int n = n_tiles;
+        const int l = seek([&](int, int upto) { return upto * n > bound; });
+        if (l < 0) return all;
+        const int mine = __builtin_amdgcn_readlane(tiles, l), each = __builtin_amdgcn_readlane(cost, l);
+        const int rest = bound - (cost_before + __builtin_amdgcn_readlane(cost_upto, l) - each) * n;
+        const int behind = (rest % each + FULL - 1) / FULL;       // token tiles that start before the bound
+        return (tiles_before + __builtin_amdgcn_readlane(tiles_upto, l) - mine) * n + rest / each * mine + min(behind, mine);
+    }
+    // Range [at, stop) of XCD `xcd`.
+    __device__ __forceinline__ int range(int xcd)
+    {
+        int all_cost = 0, all = 0;
+        for (e0 = 0; e0 < E; e0 += kWave) {
+            chunk(e0, all, all_cost);
+            all += chunk_tiles();
+            all_cost += chunk_cost();
+            if (E <= kWave) break;
+        }
+        all *= n_tiles;
+        all_cost *= n_tiles;
+        auto bound = [&](int x) { return all_cost / 8 * x + all_cost % 8 * x / 8; };
+        const int stop = xcd == 7 ? all : first_at(bound(xcd + 1), all);
+        at = first_at(bound(xcd), all);
+        return stop;
+    }
+    // The most tiles that a range can have: M tokens cost FULL for each BM of them and, the last tile of each expert, at most 3 more;
+    // the cheapest tile costs 3.
+    static int64_t most_in_a_range(int64_t M, int64_t E, int64_t n_tiles)
+    {
+        const int64_t cost = (M * FULL / BM + 1 + 3 * std::min(E, M)) * n_tiles;
+        return (cost / 8 + 2) / 3 + 1;
+    }
+    __device__ __forceinline__ void tile(int number, ExpertTile& out, int& tile_n)
+    {
+        const int n = n_tiles;
+        const int l = seek([&](int upto, int) { return upto * n > number; });
+        const int mine = __builtin_amdgcn_readlane(tiles, l);
+        const int place = number - (tiles_before + __builtin_amdgcn_readlane(tiles_upto, l) - mine) * n;
+        tile_n = place / mine;
+        out.tiles = mine;
+        out.index = place % mine;
+        out.expert = e0 + l;
+        out.row0 = __builtin_amdgcn_readlane(first, l) + out.index * BM;
+        out.end = __builtin_amdgcn_readlane(end, l);
+    }
+};
 
 typedef short short4v __attribute__((ext_vector_type(4)));
 // Four values of one column from 16 lanes' rows of four: lane 4 r + c of 16 points at columns 4 c .. 4 c + 3 of row r, lane i gets

@@ -11,8 +11,7 @@
 // transposing LDS reads, 4 rows x 16 columns for 16 lanes.  Nothing is transposed in memory, and the signs and scales are those of
 // the forward layout.
 //
-// Workgroup -> tile: the XCD w % 8 takes a contiguous range of the tiles, which are numbered expert by expert, then by output
-// tile, then by token tile, so that the CUs of an XCD share panels of W_b in its L2.
+// Workgroup -> tile: see ExpertTiles; XCD w % 8, and there tile w / 8 of its range.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,11 +22,12 @@
 
 namespace pdelta {
 
+
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
-// behind the stages: a wave's signs (1 KB: forward, its 32 rows for four steps; GRAD, its 8 rows of 256 inputs), and its scales (1 KB:
-// forward column mode, four steps' v; GRAD row mode, its 8 rows')
-constexpr int kTileLds = 2 * (kTileM * kTileK * 2 + kWBytes) + 8 * 2048;
+// behind the stages: a wave's signs (2 KB: forward, its 32 rows for two groups of four steps; GRAD, its 8 rows of 256 inputs for two
+// steps), and its scales (1 KB: forward column mode, v for two groups of four steps; GRAD row mode, its 8 rows' for two steps)
+constexpr int kTileSigns = 2 * (kTileM * kTileK * 2 + kWBytes), kTileScales = kTileSigns + 8 * 2048, kTileLds = kTileScales + 8 * 1024;
 
 struct TileArgs {
     const uint16_t* A;
@@ -46,7 +46,8 @@ template <int WDT, int AXIS, bool GRAD, int FM>
 __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile& t, int tile_n, unsigned char* tile_smem)
 {
     constexpr int BM = FM * 64, FN = 2, AQ = FM;      // tokens; MFMA tiles of a wave along outputs; load instructions of a wave for the tokens
-    constexpr int AB = BM * kTileK * 2, STAGE = AB + kWBytes, SIGNS = 2 * STAGE, SCALES = SIGNS + 8 * 1024;
+    constexpr int AB = BM * kTileK * 2, STAGE = AB + kWBytes;
+    constexpr int AHEAD = FM <= (GRAD || AXIS == 0 ? 3 : 2) ? 2 : 1;   // steps of W_b in registers, as many as there are free: see request_w
     const uint16_t *A = g.A, *v = g.v;
     const float* inverse = g.inverse;
     const int lda = g.lda, d_out = g.d_out, d_in = g.d_in, y_dtype = g.y_dtype;
@@ -103,44 +104,65 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             if constexpr (AXIS == 0) vrow[q] = (uint32_t)scales[n0 + row] * 0x10001u;
         }
         // lanes 0-31: sign words of the wave's rows for two steps, lanes 32-63 for the next two
-        soff = (uint32_t)(min(n0 + wave * 32 + (lane & 31), d_out - 1) - n0) * (uint32_t)(d_in >> 3) + (lane >> 5) * 16u;
+        soff = (uint32_t)(min(n0 + wave * 32 + (lane & 31), d_out - 1) - n0) * (uint32_t)(d_in >> 3);
     }
 
-    auto request = [&](int s, uint32_t stage) {
-        const int kb = s * kTileK;
+    // Where step s is in the contraction.  Forward, with one token tile: the output tiles start at different places of d_in, since rows
+    // of W_b are often a power of two apart and the same inputs of all rows then in few of the memory's channels (16 experts of 64
+    // tokens, 4096 x 4096 fp16: 138 -> 115 us).  With more of them the tokens are better read by all at once (2048 tokens of one
+    // expert, 8192 x 4096: 131 and 135).
+    const int start = GRAD || t.tiles > 1 ? 0 : tile_n * 2 % n_steps;
+    auto place = [&](int s) {
+        if constexpr (GRAD) return s;
+        s += start;
+        return s >= n_steps ? s - n_steps : s;
+    };
+    // Signs and scales.  Forward: for the four steps from s on (a row's last 16 bytes again behind its end).
+    const uint32_t my_signs = lds0 + kTileSigns + wave * 2048, my_scales = lds0 + kTileScales + wave * 1024;
+    auto request_signs = [&](int s) {
         if constexpr (GRAD) {
-            // rows behind the last one repeat it: the tokens are zero there
-            const int k0 = min(kb, d_out - 1);
-            auto row = [&](int r) { return (uint32_t)(min(kb + r, d_out - 1) - k0); };
-            load_lds_4(lds0 + SIGNS + wave * 1024, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
+            const int k0 = min(s * kTileK, d_out - 1);            // rows behind the last one repeat it: the tokens are zero there
+            auto row = [&](int r) { return (uint32_t)(min(s * kTileK + r, d_out - 1) - k0); };
+            load_lds_4(my_signs + (s & 1) * 256, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
             if constexpr (AXIS == 0)
-                if (lane < 8) load_lds_2(lds0 + SCALES + wave * 1024, row(wave * 8 + lane) * 2u, scales + k0);
+                if (lane < 8) load_lds_2(my_scales + (s & 1) * 32, row(wave * 8 + lane) * 2u, scales + k0);
+        } else {
+            const int group = (s >> 2) & 1;
+            load_lds_16(my_signs + group * 1024, soff + (uint32_t)place(min(s + (lane >> 5) * 2, n_steps - 2)) * 8u, sbase);
+            if constexpr (AXIS == 1)
+                if (lane < 32) load_lds_16(my_scales + group * 512, (uint32_t)(place(min(s + (lane >> 3), n_steps - 1)) * 64 + (lane & 7) * 8) * 2u, scales);
+        }
+    };
+    auto request_a = [&](int s, uint32_t stage) {
+#pragma unroll
+        for (int q = 0; q < AQ; ++q) load_lds_16(lds0 + stage + (wave * AQ + q) * 1024, aoff[q], abase + (int64_t)place(s) * (kTileK * 2));
+    };
+    // W_b goes through registers, AHEAD steps of it: it comes out of HBM, and with loads into the two LDS stages, which are free for
+    // half a step only, a step took twice the memory's latency.
+    uint4v raw[AHEAD][4];
+    auto request_w = [&](int s, auto which) {
+        uint4v(&into)[4] = raw[decltype(which)::value % AHEAD];
+        if constexpr (GRAD) {
+            const int k0 = min(s * kTileK, d_out - 1);
+            const char* base = wbase + (int64_t)k0 * d_in * 2;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                load_lds_16(lds0 + stage + AB + (wave * 4 + q) * 1024, row(wave * 8 + q * 2 + (lane >> 5)) * (uint32_t)d_in * 2u + woff[q & 1],
-                            wbase + (int64_t)k0 * d_in * 2);
+                into[q] = *(const uint4v*)(base + ((uint32_t)(min(s * kTileK + wave * 8 + q * 2 + (lane >> 5), d_out - 1) - k0) * (uint32_t)d_in * 2u + woff[q & 1]));
         } else {
-            if ((s & 3) == 0) {                       // never past d_in: a short last group repeats its first half
-                load_lds_16(lds0 + SIGNS + wave * 1024, kb + 128 < d_in ? soff : soff - (lane >> 5) * 16u, sbase + (kb >> 3));
-                if constexpr (AXIS == 1)
-                    load_lds_16(lds0 + SCALES + wave * 1024, (uint32_t)min(kb + (lane & 31) * 8, d_in - 8) * 2u, scales);
-            }
+            const char* base = wbase + (int64_t)place(s) * (kTileK * 2);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) load_lds_16(lds0 + stage + AB + (wave * 4 + q) * 1024, woff[q], wbase + (int64_t)kb * 2);
+            for (int q = 0; q < 4; ++q) into[q] = *(const uint4v*)(base + woff[q]);
         }
-#pragma unroll
-        for (int q = 0; q < AQ; ++q) load_lds_16(lds0 + stage + (wave * AQ + q) * 1024, aoff[q], abase + (int64_t)kb * 2);
     };
 
-    // In place: the wave's own pieces of W_b -> W_hat.
-    uint4v raw[4], wvec[2];
+    // The lane's pieces of W_b -> W_hat in LDS.
+    uint4v wvec[2];
     uint32_t sbyte[4], wscale[4];
-    auto fetch_w = [&](int s, uint32_t stage) {
-        const unsigned char* sg = tile_smem + SIGNS + wave * 1024;
-        const unsigned char* sc = tile_smem + SCALES + wave * 1024;
+    auto fetch_signs = [&](int s) {
+        const unsigned char* sg = tile_smem + kTileSigns + wave * 2048 + (GRAD ? (s & 1) * 256 : ((s >> 2) & 1) * 1024);
+        const unsigned char* sc = tile_smem + kTileScales + wave * 1024 + (GRAD ? (s & 1) * 32 : ((s >> 2) & 1) * 512);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            raw[q] = *(const uint4v*)(tile_smem + stage + AB + (wave * 4 + q) * 1024 + lane * 16);
             if constexpr (GRAD) {
                 sbyte[q] = sg[(q * 2 + (lane >> 5)) * 32 + chunk[q & 1]];
                 if constexpr (AXIS == 0) wscale[q] = *(const uint16_t*)(sc + (q * 2 + (lane >> 5)) * 4);
@@ -153,7 +175,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             for (int q = 0; q < 2; ++q) wvec[q] = *(const uint4v*)(sc + (s & 3) * 128 + chunk[q] * 16);
         }
     };
-    auto convert_w = [&](uint32_t stage) {
+    auto convert_w = [&](uint32_t stage, auto which) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint32_t minus = ~sbyte[q] & 0xFFu;
@@ -161,7 +183,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             asm("" : "+v"(y));                        // (else y and its shifts become full multiplications)
             uint32_t vv = 0;
             if constexpr (AXIS == 0) vv = GRAD ? wscale[q] | (wscale[q] << 16) : vrow[q];
-            const uint4v w16 = to_f16x8<WDT>(raw[q]);
+            const uint4v w16 = to_f16x8<WDT>(raw[decltype(which)::value % AHEAD][q]);
             uint4v r;
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
@@ -191,7 +213,9 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     half8 a[2][FM], b[2][FN];
     auto read_frags = [&](uint32_t stage, auto step16) {
         constexpr int ks = decltype(step16)::value;
-        const uint32_t at = frag ^ (uint32_t)(ks * 32);
+        uint32_t at = frag ^ (uint32_t)(ks * 32);
+        // (where registers are short: computed here, not kept)
+        if constexpr (FM == 4 && AXIS == 1 && !GRAD) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "n"(ks * 32), "v"(frag));
         const unsigned char* xa = tile_smem + stage + wm * (BM / 2) * 128 + at;
 #pragma unroll
         for (int h = 0; h < FN; ++h) {
@@ -214,49 +238,67 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
                 acc[f][h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[ks & 1][f], b[ks & 1][h], acc[f][h], 0, 0, 0);
     };
 
-    request(0, 0);
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    request_signs(0);
+    if constexpr (GRAD) request_signs(1);
+    request_a(0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    request_w(0, I0{});
+    if constexpr (AHEAD == 2) request_w(1, I1{});
     wait_loads<0>();
-    fetch_w(0, 0);
-    convert_w(0);
+    fetch_signs(0);
+    convert_w(0, I0{});
     lds_barrier();
-    request(1, STAGE);
-    read_frags(0, std::integral_constant<int, 0>{});
+    request_a(1, STAGE);
+    __builtin_amdgcn_sched_barrier(0);
+    request_w(min(AHEAD, n_steps - 1), I0{});
+    read_frags(0, I0{});
 
-    // Step s; REQ: request step s + 2, MORE: there is a step s + 1.  The fences keep the LDS reads above the MFMAs and the
-    // conversion between them.
-    auto step = [&](int s, uint32_t cur, uint32_t nxt, auto req, auto more) {
+    // Step s.  What is asked for in its last quarter: the signs, then the tokens of step s + 2, then W_b of step s + 1 + AHEAD; in the
+    // next step's first quarter all but those last four loads have to be there.  REQ: there is a step s + 2, MORE: a step s + 1.
+    // The fences keep the LDS reads above the MFMAs, the conversion between them, and the loads in their order.
+    auto step = [&](int s, uint32_t cur, uint32_t nxt, auto next, auto req, auto more) {
         constexpr bool REQ = decltype(req)::value, MORE = decltype(more)::value;
         constexpr int VALU = ((WDT == kBF16 ? 13 : 7) * 8 + FM * FN - 1) / (FM * FN);     // vector instructions after each MFMA of a quarter
-        read_frags(cur, std::integral_constant<int, 1>{});
+        read_frags(cur, I1{});
         __builtin_amdgcn_sched_barrier(0);
         multiply(0);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE) wait_loads<AQ>();         // (the last ones are the tokens')
-        if constexpr (MORE) fetch_w(s + 1, nxt);
+        if constexpr (MORE) {
+            wait_loads<AHEAD == 2 ? 4 : 0>();
+            fetch_signs(s + 1);
+        }
         read_frags(cur, std::integral_constant<int, 2>{});
         __builtin_amdgcn_sched_barrier(0);
         multiply(1);
-        if constexpr (MORE) { convert_w(nxt); interleave<FM * FN, VALU>(); }
+        if constexpr (MORE) { convert_w(nxt, next); interleave<FM * FN, VALU>(); }
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (REQ && AHEAD == 1) request_w(s + 2, I0{});
         read_frags(cur, std::integral_constant<int, 3>{});
         __builtin_amdgcn_sched_barrier(0);
         multiply(2);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE) wait_loads<0>();
         lds_barrier();
-        if constexpr (MORE) read_frags(nxt, std::integral_constant<int, 0>{});
-        if constexpr (REQ) request(s + 2, cur);
+        if constexpr (MORE) read_frags(nxt, I0{});
+        if constexpr (REQ) {
+            if constexpr (GRAD) request_signs(s + 2);
+            else if ((s & 3) == 0) request_signs(s + 4);
+            request_a(s + 2, cur);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (AHEAD == 2) request_w(min(s + 3, n_steps - 1), next);
+        }
         __builtin_amdgcn_sched_barrier(0);
         multiply(3);
         __builtin_amdgcn_sched_barrier(0);
     };
     int s = 0;
     for (; s + 2 < n_steps; s += 2) {
-        step(s, 0, STAGE, std::true_type{}, std::true_type{});
-        step(s + 1, STAGE, 0, std::true_type{}, std::true_type{});
+        step(s, 0, STAGE, I1{}, std::true_type{}, std::true_type{});
+        step(s + 1, STAGE, 0, I0{}, std::true_type{}, std::true_type{});
     }
-    step(s, 0, STAGE, std::false_type{}, std::true_type{});
-    step(s + 1, STAGE, 0, std::false_type{}, std::false_type{});
+    step(s, 0, STAGE, I1{}, std::false_type{}, std::true_type{});
+    step(s + 1, STAGE, 0, I0{}, std::false_type{}, std::false_type{});
 
     // (the last barrier came after the last fragment read: the stages are free)
     const int m0 = t.row0 + wm * (BM / 2);
@@ -281,10 +323,15 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
                    const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out, int d_in, int y_dtype, int n_tiles)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
+    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, d_out, d_in, y_dtype};
     ExpertTile t;
     int tile_n;
-    if (!find_expert_block<kTileM>(offsets, E, M, n_tiles, (int)blockIdx.x % kXcds, (int)blockIdx.x / kXcds, t, tile_n)) return;  // whole workgroup
-    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, d_out, d_in, y_dtype};
+    {
+        ExpertTiles<kTileM> list{offsets, E, M, n_tiles};
+        const int stop = list.range((int)blockIdx.x % kXcds), number = list.at + (int)blockIdx.x / kXcds;
+        if (number >= stop) return;                   // whole workgroup
+        list.tile(number, t, tile_n);
+    }
     const int rows = t.end - t.row0;
     if (rows > 192) experts_tile<WDT, AXIS, GRAD, 4>(g, t, tile_n, tile_smem);
     else if (rows > 128) experts_tile<WDT, AXIS, GRAD, 3>(g, t, tile_n, tile_smem);
@@ -297,8 +344,8 @@ static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, co
 {
     constexpr int lds = kTileLds;
     const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
-    const int64_t blocks = (most_expert_tiles(c.M, c.E, kTileM) * n_tiles + kXcds - 1) / kXcds * kXcds;
-    if (blocks > 0x7FFFFFFF) return -2;
+    const int64_t most = ExpertTiles<kTileM>::most_in_a_range(c.M, c.E, n_tiles), blocks = most * kXcds;
+    if (most > (1 << 24)) return -2;                  // (costs are summed in 32 bits)
     auto kernel = experts_big_kernel<WDT, AXIS, GRAD>;
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
