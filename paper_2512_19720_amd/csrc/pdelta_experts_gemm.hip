@@ -179,6 +179,13 @@ static size_t prepared_bytes(int64_t M, int64_t K, int dtype)
     if (!needs_prepare(K, dtype)) return 0;
     return (size_t)M * (size_t)experts_padded(K) * 2 + ((size_t)M * 4 + 15) / 16 * 16;
 }
+// Whether the tiles with direct loads take a product whose contraction is K long.
+static bool takes_big(bool grad, int64_t K) { return grad || (K & 127) == 0; }
+static size_t product_bytes(bool grad, int64_t M, int64_t E, int64_t N, int64_t K, int dtype)
+{
+    const int64_t parts = takes_big(grad, K) ? experts_parts(M, E, N, K) : 1;
+    return prepared_bytes(M, K, dtype) + (parts > 1 ? (size_t)(parts * M * N) * 4 : 0);
+}
 
 template <int WDT, int AXIS, bool GRAD>
 static int launch_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
@@ -211,7 +218,11 @@ static int launch_product(const ExpertsCall& c, bool grad, hipStream_t stream)
         }
         A = rows;
     }
-    if (grad || (K & 127) == 0) return launch_experts_big(c, grad, A, lda, inverse, stream);
+    if (takes_big(grad, K)) {
+        const int64_t N = grad ? c.d_in : c.d_out;
+        return launch_experts_big(c, grad, A, lda, inverse, (float*)((char*)c.workspace + prepared_bytes(c.M, K, c.dtype)),
+                                  experts_parts(c.M, c.E, N, K), stream);
+    }
 #define PDELTA_GO(WDT, AXIS) \
     return grad ? launch_tiles<WDT, AXIS, true>(c, A, lda, inverse, stream) : launch_tiles<WDT, AXIS, false>(c, A, lda, inverse, stream)
     if (c.dtype == kBF16) {
@@ -223,9 +234,19 @@ static int launch_product(const ExpertsCall& c, bool grad, hipStream_t stream)
 #undef PDELTA_GO
 }
 
-size_t experts_linear_workspace_bytes(int64_t M, int64_t, int64_t, int64_t d_in, int dtype) { return prepared_bytes(M, d_in, dtype); }
-size_t experts_grad_x_workspace_bytes(int64_t M, int64_t, int64_t d_out, int64_t, int dtype) { return prepared_bytes(M, d_out, dtype); }
-int launch_experts_linear(const ExpertsCall& c, hipStream_t stream) { return launch_product(c, false, stream); }
+size_t experts_linear_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
+{
+    return experts_decode_tokens(M, E, d_out, d_in, dtype) > 0 ? 0 : product_bytes(false, M, E, d_out, d_in, dtype);
+}
+size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
+{
+    return product_bytes(true, M, E, d_in, d_out, dtype);
+}
+int launch_experts_linear(const ExpertsCall& c, hipStream_t stream)
+{
+    const int mt = experts_decode_tokens(c.M, c.E, c.d_out, c.d_in, c.dtype);
+    return mt > 0 ? launch_experts_skinny(c, mt, stream) : launch_product(c, false, stream);
+}
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream) { return launch_product(c, true, stream); }
 
 }  // namespace pdelta

@@ -25,9 +25,9 @@ namespace pdelta {
 
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
-// behind the stages: a wave's signs (2 KB: forward, its 32 rows for two groups of four steps; GRAD, its 8 rows of 256 inputs for two
-// steps), and its scales (1 KB: forward column mode, v for two groups of four steps; GRAD row mode, its 8 rows' for two steps)
-constexpr int kTileSigns = 2 * (kTileM * kTileK * 2 + kWBytes), kTileScales = kTileSigns + 8 * 2048, kTileLds = kTileScales + 8 * 1024;
+// behind the stages: a wave's signs (2 KB: forward, its 32 rows for two groups of four steps; GRAD, its 8 rows of 256 inputs for
+// four steps), and its scales (1 KB: forward column mode, v for two groups of four steps; GRAD row mode, its 8 rows' for four)
+constexpr int kTileW = 2 * kTileM * kTileK * 2, kTileSigns = kTileW + 2 * kWBytes, kTileScales = kTileSigns + 8 * 2048, kTileLds = kTileScales + 8 * 1024;
 
 struct TileArgs {
     const uint16_t* A;
@@ -38,22 +38,32 @@ struct TileArgs {
     const uint32_t* B_packed;
     const uint16_t* v;
     void* Y;
-    int d_out, d_in, y_dtype;
+    float* partial;
+    int M, d_out, d_in, y_dtype, parts;
 };
 
 // One tile of 64 FM tokens, waves of 32 FM x 64 outputs.
 template <int WDT, int AXIS, bool GRAD, int FM>
-__device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile& t, int tile_n, unsigned char* tile_smem)
+__device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile& t, int tile_n, int part, unsigned char* tile_smem)
 {
     constexpr int BM = FM * 64, FN = 2, AQ = FM;      // tokens; MFMA tiles of a wave along outputs; load instructions of a wave for the tokens
-    constexpr int AB = BM * kTileK * 2, STAGE = AB + kWBytes;
-    constexpr int AHEAD = FM <= (GRAD || AXIS == 0 ? 3 : 2) ? 2 : 1;   // steps of W_b in registers, as many as there are free: see request_w
+    // Up to 128 tokens four steps of tokens are on their way in LDS and four of W_b in registers: a step is then shorter than the
+    // memory's latency.  Larger tiles: two, and as many steps of W_b as there are registers free.
+    constexpr bool DEEP = FM <= 2;
+    constexpr int STEPS = DEEP ? 4 : 2, AHEAD = DEEP ? 4 : FM == 3 && (GRAD || AXIS == 0) ? 2 : 1;
+    constexpr int AB = BM * kTileK * 2;
+    auto a_stage = [](int s) { return (uint32_t)(s % STEPS * AB); };
+    auto w_stage = [](int s) { return (uint32_t)(kTileW + s % 2 * kWBytes); };
     const uint16_t *A = g.A, *v = g.v;
-    const float* inverse = g.inverse;
-    const int lda = g.lda, d_out = g.d_out, d_in = g.d_in, y_dtype = g.y_dtype;
-    void* Y = g.Y;
+    // (a part leaves its sums as they are; experts_sum_kernel does the rest)
+    const float* inverse = g.parts > 1 ? nullptr : g.inverse;
+    const int lda = g.lda, d_out = g.d_out, d_in = g.d_in, y_dtype = g.parts > 1 ? kF32 : g.y_dtype;
+    void* Y = g.parts > 1 ? (void*)(g.partial + (int64_t)part * g.M * (GRAD ? g.d_in : g.d_out)) : g.Y;
     const int N = GRAD ? d_in : d_out;
-    const int n0 = tile_n * kTileN, n_steps = lda / kTileK;       // even, at least 2
+    const int n0 = tile_n * kTileN;
+    // the steps of this part of the contraction: an even number of them, at least 2
+    const int first_step = (int)((int64_t)(lda / kTileK / 2) * part / g.parts) * 2;
+    const int n_steps = (int)((int64_t)(lda / kTileK / 2) * (part + 1) / g.parts) * 2 - first_step;
     const uint16_t* W = g.W_b + t.expert * g.w_stride;
     const uint32_t* B = g.B_packed + (int64_t)t.expert * d_out * (d_in / 32);
     const uint16_t* scales = v + (int64_t)t.expert * (AXIS == 0 ? d_out : d_in);
@@ -109,23 +119,23 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
 
     // Where step s is in the contraction.  Forward, with one token tile: the output tiles start at different places of d_in, since rows
     // of W_b are often a power of two apart and the same inputs of all rows then in few of the memory's channels (16 experts of 64
-    // tokens, 4096 x 4096 fp16: 138 -> 115 us).  With more of them the tokens are better read by all at once (2048 tokens of one
+    // tokens, 4096 x 4096 fp16: 138 -> 117 us).  With more of them the tokens are better read by all at once (2048 tokens of one
     // expert, 8192 x 4096: 131 and 135).
-    const int start = GRAD || t.tiles > 1 ? 0 : tile_n * 2 % n_steps;
+    const int start = GRAD || t.tiles > 1 ? 0 : (tile_n + (g.w_stride != 0 ? t.expert * 5 : 0)) * 6 % n_steps / 2 * 2;
     auto place = [&](int s) {
-        if constexpr (GRAD) return s;
+        if constexpr (GRAD) return first_step + s;
         s += start;
-        return s >= n_steps ? s - n_steps : s;
+        return first_step + (s >= n_steps ? s - n_steps : s);
     };
     // Signs and scales.  Forward: for the four steps from s on (a row's last 16 bytes again behind its end).
     const uint32_t my_signs = lds0 + kTileSigns + wave * 2048, my_scales = lds0 + kTileScales + wave * 1024;
     auto request_signs = [&](int s) {
         if constexpr (GRAD) {
-            const int k0 = min(s * kTileK, d_out - 1);            // rows behind the last one repeat it: the tokens are zero there
-            auto row = [&](int r) { return (uint32_t)(min(s * kTileK + r, d_out - 1) - k0); };
-            load_lds_4(my_signs + (s & 1) * 256, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
+            const int kb = place(s) * kTileK, k0 = min(kb, d_out - 1);        // rows behind the last one repeat it: the tokens are zero there
+            auto row = [&](int r) { return (uint32_t)(min(kb + r, d_out - 1) - k0); };
+            load_lds_4(my_signs + (s & 3) * 256, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
             if constexpr (AXIS == 0)
-                if (lane < 8) load_lds_2(my_scales + (s & 1) * 32, row(wave * 8 + lane) * 2u, scales + k0);
+                if (lane < 8) load_lds_2(my_scales + (s & 3) * 32, row(wave * 8 + lane) * 2u, scales + k0);
         } else {
             const int group = (s >> 2) & 1;
             load_lds_16(my_signs + group * 1024, soff + (uint32_t)place(min(s + (lane >> 5) * 2, n_steps - 2)) * 8u, sbase);
@@ -138,16 +148,16 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
         for (int q = 0; q < AQ; ++q) load_lds_16(lds0 + stage + (wave * AQ + q) * 1024, aoff[q], abase + (int64_t)place(s) * (kTileK * 2));
     };
     // W_b goes through registers, AHEAD steps of it: it comes out of HBM, and with loads into the two LDS stages, which are free for
-    // half a step only, a step took twice the memory's latency.
+    // half a step only, a step took twice the memory's latency (16 experts of 64 tokens, 4096 x 4096 fp16, input gradient: 123 -> 96 us).
     uint4v raw[AHEAD][4];
     auto request_w = [&](int s, auto which) {
         uint4v(&into)[4] = raw[decltype(which)::value % AHEAD];
         if constexpr (GRAD) {
-            const int k0 = min(s * kTileK, d_out - 1);
+            const int kb = place(s) * kTileK, k0 = min(kb, d_out - 1);
             const char* base = wbase + (int64_t)k0 * d_in * 2;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                into[q] = *(const uint4v*)(base + ((uint32_t)(min(s * kTileK + wave * 8 + q * 2 + (lane >> 5), d_out - 1) - k0) * (uint32_t)d_in * 2u + woff[q & 1]));
+                into[q] = *(const uint4v*)(base + ((uint32_t)(min(kb + wave * 8 + q * 2 + (lane >> 5), d_out - 1) - k0) * (uint32_t)d_in * 2u + woff[q & 1]));
         } else {
             const char* base = wbase + (int64_t)place(s) * (kTileK * 2);
 #pragma unroll
@@ -159,8 +169,8 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     uint4v wvec[2];
     uint32_t sbyte[4], wscale[4];
     auto fetch_signs = [&](int s) {
-        const unsigned char* sg = tile_smem + kTileSigns + wave * 2048 + (GRAD ? (s & 1) * 256 : ((s >> 2) & 1) * 1024);
-        const unsigned char* sc = tile_smem + kTileScales + wave * 1024 + (GRAD ? (s & 1) * 32 : ((s >> 2) & 1) * 512);
+        const unsigned char* sg = tile_smem + kTileSigns + wave * 2048 + (GRAD ? (s & 3) * 256 : ((s >> 2) & 1) * 1024);
+        const unsigned char* sc = tile_smem + kTileScales + wave * 1024 + (GRAD ? (s & 3) * 32 : ((s >> 2) & 1) * 512);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if constexpr (GRAD) {
@@ -192,7 +202,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
                 const uint32_t wp = w16[p], sv = ((y << (15 - 2 * p)) & 0x80008000u) ^ vp;      // -v where the bit is set
                 r[p] = as_u32(as_half2(wp) + as_half2(sv));
             }
-            *(uint4v*)(tile_smem + stage + AB + (wave * 4 + q) * 1024 + lane * 16) = r;
+            *(uint4v*)(tile_smem + stage + (wave * 4 + q) * 1024 + lane * 16) = r;
         }
     };
 
@@ -211,20 +221,20 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     const uint32_t tfrag = (uint32_t)((lane >> 5) * 8 + tr) * 512u +
                            ((uint32_t)(wn * 128 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8) ^ (uint32_t)(tr << 6));
     half8 a[2][FM], b[2][FN];
-    auto read_frags = [&](uint32_t stage, auto step16) {
+    auto read_frags = [&](uint32_t as, uint32_t ws, auto step16) {
         constexpr int ks = decltype(step16)::value;
         uint32_t at = frag ^ (uint32_t)(ks * 32);
         // (where registers are short: computed here, not kept)
         if constexpr (FM == 4 && AXIS == 1 && !GRAD) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "n"(ks * 32), "v"(frag));
-        const unsigned char* xa = tile_smem + stage + wm * (BM / 2) * 128 + at;
+        const unsigned char* xa = tile_smem + as + wm * (BM / 2) * 128 + at;
 #pragma unroll
         for (int h = 0; h < FN; ++h) {
             if constexpr (GRAD) {
-                const unsigned char* p = tile_smem + stage + AB + ks * 16 * 512 + (tfrag ^ (uint32_t)(h * 64));
+                const unsigned char* p = tile_smem + ws + ks * 16 * 512 + (tfrag ^ (uint32_t)(h * 64));
                 const uint2v lo = read_transposed(p), hi = read_transposed(p + 4 * 512);
                 b[ks & 1][h] = __builtin_bit_cast(half8, (uint4v){lo[0], lo[1], hi[0], hi[1]});
             } else {
-                b[ks & 1][h] = *(const half8*)(tile_smem + stage + AB + wn * 64 * 128 + at + h * 32 * 128);
+                b[ks & 1][h] = *(const half8*)(tile_smem + ws + wn * 64 * 128 + at + h * 32 * 128);
             }
         }
 #pragma unroll
@@ -240,65 +250,141 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
 
     using I0 = std::integral_constant<int, 0>;
     using I1 = std::integral_constant<int, 1>;
-    request_signs(0);
-    if constexpr (GRAD) request_signs(1);
-    request_a(0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    request_w(0, I0{});
-    if constexpr (AHEAD == 2) request_w(1, I1{});
-    wait_loads<0>();
-    fetch_signs(0);
-    convert_w(0, I0{});
-    lds_barrier();
-    request_a(1, STAGE);
-    __builtin_amdgcn_sched_barrier(0);
-    request_w(min(AHEAD, n_steps - 1), I0{});
-    read_frags(0, I0{});
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    constexpr int VALU = ((WDT == kBF16 ? 13 : 7) * 8 + FM * FN - 1) / (FM * FN);     // vector instructions after each MFMA of a quarter
+    const int last = n_steps - 1;
 
-    // Step s.  What is asked for in its last quarter: the signs, then the tokens of step s + 2, then W_b of step s + 1 + AHEAD; in the
-    // next step's first quarter all but those last four loads have to be there.  REQ: there is a step s + 2, MORE: a step s + 1.
-    // The fences keep the LDS reads above the MFMAs, the conversion between them, and the loads in their order.
-    auto step = [&](int s, uint32_t cur, uint32_t nxt, auto next, auto req, auto more) {
-        constexpr bool REQ = decltype(req)::value, MORE = decltype(more)::value;
-        constexpr int VALU = ((WDT == kBF16 ? 13 : 7) * 8 + FM * FN - 1) / (FM * FN);     // vector instructions after each MFMA of a quarter
-        read_frags(cur, I1{});
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(0);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (MORE) {
-            wait_loads<AHEAD == 2 ? 4 : 0>();
-            fetch_signs(s + 1);
+    // The fences keep the LDS reads above the MFMAs, the conversion between them, and the loads in their order: a wait counts the
+    // loads asked for since.
+    if constexpr (DEEP) {
+        // The first loads of all four steps.  Behind the last step the last one's are asked for again, into places that nobody reads.
+        request_signs(0);
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int k = 1; k < 4; ++k) request_signs(k);
         }
-        read_frags(cur, std::integral_constant<int, 2>{});
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1);
-        if constexpr (MORE) { convert_w(nxt, next); interleave<FM * FN, VALU>(); }
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (REQ && AHEAD == 1) request_w(s + 2, I0{});
-        read_frags(cur, std::integral_constant<int, 3>{});
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(2);
-        __builtin_amdgcn_sched_barrier(0);
-        lds_barrier();
-        if constexpr (MORE) read_frags(nxt, I0{});
-        if constexpr (REQ) {
-            if constexpr (GRAD) request_signs(s + 2);
-            else if ((s & 3) == 0) request_signs(s + 4);
-            request_a(s + 2, cur);
+        auto first = [&](auto k) {
+            request_a(min((int)decltype(k)::value, last), a_stage(decltype(k)::value));
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (AHEAD == 2) request_w(min(s + 3, n_steps - 1), next);
+            request_w(min((int)decltype(k)::value, last), k);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        first(I0{});
+        first(I1{});
+        first(I2{});
+        first(I3{});
+        wait_loads<0>();
+        fetch_signs(0);
+        convert_w(w_stage(0), I0{});
+        lds_barrier();
+        request_w(min(4, last), I0{});
+        read_frags(a_stage(0), w_stage(0), I0{});
+
+        // Step s, s % 4 = P.  In its last quarter the signs and the tokens of step s + 4 and W_b of step s + 5 are asked for; what the
+        // next step needs is then behind at least three steps' W_b, 12 loads.
+        auto step = [&](int s, auto phase) {
+            constexpr int P = decltype(phase)::value;
+            using Next = std::integral_constant<int, (P + 1) % 4>;
+            read_frags(a_stage(P), w_stage(P), I1{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_loads<12>();
+            fetch_signs(s + 1);
+            read_frags(a_stage(P), w_stage(P), I2{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+            convert_w(w_stage(P + 1), Next{});
+            interleave<FM * FN, VALU>();
+            __builtin_amdgcn_sched_barrier(0);
+            read_frags(a_stage(P), w_stage(P), I3{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(2);
+            __builtin_amdgcn_sched_barrier(0);
+            lds_barrier();
+            read_frags(a_stage(P + 1), w_stage(P + 1), I0{});
+            if constexpr (GRAD) request_signs(s + 4);
+            else if constexpr (P == 0) request_signs(s + 4);
+            request_a(min(s + 4, last), a_stage(P));
+            __builtin_amdgcn_sched_barrier(0);
+            request_w(min(s + 5, last), Next{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(3);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int s = 0; s < n_steps; s += 4) {
+            step(s, I0{});
+            step(s + 1, I1{});
+            if (s + 2 < n_steps) {                    // uniform
+                step(s + 2, I2{});
+                step(s + 3, I3{});
+            }
         }
+        wait_loads<0>();
+        lds_barrier();                                // nothing is on its way into LDS any more
+    } else {
+        request_signs(0);
+        if constexpr (GRAD) request_signs(1);
+        request_a(0, a_stage(0));
         __builtin_amdgcn_sched_barrier(0);
-        multiply(3);
+        request_w(0, I0{});
+        if constexpr (AHEAD == 2) request_w(1, I1{});
+        wait_loads<0>();
+        fetch_signs(0);
+        convert_w(w_stage(0), I0{});
+        lds_barrier();
+        request_a(1, a_stage(1));
         __builtin_amdgcn_sched_barrier(0);
-    };
-    int s = 0;
-    for (; s + 2 < n_steps; s += 2) {
-        step(s, 0, STAGE, I1{}, std::true_type{}, std::true_type{});
-        step(s + 1, STAGE, 0, I0{}, std::true_type{}, std::true_type{});
+        request_w(min(AHEAD, last), I0{});
+        read_frags(a_stage(0), w_stage(0), I0{});
+
+        // Step s, s % 2 = P.  What is asked for in its last quarter: the signs, then the tokens of step s + 2, then W_b of step s + 1 +
+        // AHEAD (one step ahead: as soon as it is converted); in the next step's second quarter all but those last four loads have to
+        // be there.  REQ: there is a step s + 2, MORE: a step s + 1.
+        auto step = [&](int s, auto phase, auto req, auto more) {
+            constexpr int P = decltype(phase)::value;
+            constexpr bool REQ = decltype(req)::value, MORE = decltype(more)::value;
+            using Next = std::integral_constant<int, 1 - P>;
+            read_frags(a_stage(P), w_stage(P), I1{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (MORE) {
+                wait_loads<AHEAD == 2 ? 4 : 0>();
+                fetch_signs(s + 1);
+            }
+            read_frags(a_stage(P), w_stage(P), I2{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+            if constexpr (MORE) { convert_w(w_stage(P + 1), Next{}); interleave<FM * FN, VALU>(); }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (REQ && AHEAD == 1) request_w(s + 2, I0{});
+            read_frags(a_stage(P), w_stage(P), I3{});
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(2);
+            __builtin_amdgcn_sched_barrier(0);
+            lds_barrier();
+            if constexpr (MORE) read_frags(a_stage(P + 1), w_stage(P + 1), I0{});
+            if constexpr (REQ) {
+                if constexpr (GRAD) request_signs(s + 2);
+                else if ((s & 3) == 0) request_signs(s + 4);
+                request_a(s + 2, a_stage(P));
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (AHEAD == 2) request_w(min(s + 3, last), Next{});
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(3);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int s = 0;
+        for (; s + 2 < n_steps; s += 2) {
+            step(s, I0{}, std::true_type{}, std::true_type{});
+            step(s + 1, I1{}, std::true_type{}, std::true_type{});
+        }
+        step(s, I0{}, std::false_type{}, std::true_type{});
+        step(s + 1, I1{}, std::false_type{}, std::false_type{});
     }
-    step(s, 0, STAGE, I1{}, std::false_type{}, std::true_type{});
-    step(s + 1, STAGE, 0, I0{}, std::false_type{}, std::false_type{});
 
     // (the last barrier came after the last fragment read: the stages are free)
     const int m0 = t.row0 + wm * (BM / 2);
@@ -320,54 +406,110 @@ template <int WDT, int AXIS, bool GRAD>
 __global__ void __launch_bounds__(512, 2)
 experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
                    const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
-                   const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out, int d_in, int y_dtype, int n_tiles)
+                   const uint16_t* __restrict__ v, void* __restrict__ Y, float* __restrict__ partial, int M, int E, int d_out, int d_in, int y_dtype,
+                   int n_tiles, int parts)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
-    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, d_out, d_in, y_dtype};
+    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts};
     ExpertTile t;
     int tile_n;
     {
-        ExpertTiles<kTileM> list{offsets, E, M, n_tiles};
+        ExpertTiles<kTileM> list{offsets, E, M, n_tiles * parts};     // a part is a tile of its own here
         const int stop = list.range((int)blockIdx.x % kXcds), number = list.at + (int)blockIdx.x / kXcds;
         if (number >= stop) return;                   // whole workgroup
         list.tile(number, t, tile_n);
     }
+    const int part = tile_n % parts;
+    tile_n /= parts;
     const int rows = t.end - t.row0;
-    if (rows > 192) experts_tile<WDT, AXIS, GRAD, 4>(g, t, tile_n, tile_smem);
-    else if (rows > 128) experts_tile<WDT, AXIS, GRAD, 3>(g, t, tile_n, tile_smem);
-    else if (rows > 64) experts_tile<WDT, AXIS, GRAD, 2>(g, t, tile_n, tile_smem);
-    else experts_tile<WDT, AXIS, GRAD, 1>(g, t, tile_n, tile_smem);
+    if (rows > 192) experts_tile<WDT, AXIS, GRAD, 4>(g, t, tile_n, part, tile_smem);
+    else if (rows > 128) experts_tile<WDT, AXIS, GRAD, 3>(g, t, tile_n, part, tile_smem);
+    else if (rows > 64) experts_tile<WDT, AXIS, GRAD, 2>(g, t, tile_n, part, tile_smem);
+    else experts_tile<WDT, AXIS, GRAD, 1>(g, t, tile_n, part, tile_smem);
+}
+
+// The parts' sums of a split contraction, in their order, for rows that belong to an expert.
+template <int YDT>
+__global__ void __launch_bounds__(256)
+experts_sum_kernel(const float* __restrict__ partial, const float* __restrict__ inverse, const int* __restrict__ offsets, void* __restrict__ Y,
+                   int M, int E, int N, int parts, int blocks)
+{
+    const int m = blockIdx.x / blocks, n = (blockIdx.x % blocks * 256 + threadIdx.x) * 4;
+    if (n >= N || (offsets != nullptr && (m < offsets[0] || m >= offsets[E]))) return;
+    const float x = inverse != nullptr ? inverse[m] : 1.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const int64_t at = (int64_t)m * N + n;
+    if ((N & 3) == 0) {
+        for (int p = 0; p < parts; ++p) {
+            const float4v a = *(const float4v*)(partial + (int64_t)p * M * N + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += a[e];
+        }
+    } else {
+        for (int p = 0; p < parts; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N) sum[e] += partial[(int64_t)p * M * N + at + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < N) store_y<YDT>(Y, at + e, sum[e] * x);
+}
+
+// Parts of the contraction: tiles that leave most of the 256 CUs idle are cut into as many parts as fill them, of four steps at
+// least (one expert, 64 tokens, 4096 x 4096 fp16, 16 tiles: 52 us, in 16 parts 26; 8 experts, 128 tiles: 75, in two parts 68).  More
+// parts than that cost more than they give (12 fine-tunes, 1501 tokens, 192 tiles of unequal length: 118, in three parts 142; 16
+// experts of 64 tokens, 256 tiles: 119, in two parts 161).  The sums take at most 64 MiB of workspace.
+int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K)
+{
+    if (M == 0) return 1;
+    const int64_t met = std::min(E, M), tiles = (N + kTileN - 1) / kTileN * met * ((M + met * kTileM - 1) / (met * kTileM));
+    const int64_t steps = experts_padded(K) / kTileK;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({16, 256 / tiles, steps / 4}));
 }
 
 template <int WDT, int AXIS, bool GRAD>
-static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
+static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, float* partial, int parts, hipStream_t stream)
 {
     constexpr int lds = kTileLds;
     const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
-    const int64_t most = ExpertTiles<kTileM>::most_in_a_range(c.M, c.E, n_tiles), blocks = most * kXcds;
+    const int64_t most = ExpertTiles<kTileM>::most_in_a_range(c.M, c.E, n_tiles * parts), blocks = most * kXcds;
     if (most > (1 << 24)) return -2;                  // (costs are summed in 32 bits)
     auto kernel = experts_big_kernel<WDT, AXIS, GRAD>;
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), lds, stream, A, lda, inverse, c.offsets, (const uint16_t*)c.W_b, c.w_stride,
-                       c.B_packed, c.v, c.out, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles);
+                       c.B_packed, c.v, c.out, partial, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles, parts);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, hipStream_t stream)
+int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, float* partial, int parts,
+                       hipStream_t stream)
 {
-#define PDELTA_GO(WDT, AXIS, GRAD) return launch_big_tiles<WDT, AXIS, GRAD>(c, A, lda, inverse, stream)
-    if (c.dtype == kBF16) {
-        if (c.axis == 0 && grad) PDELTA_GO(kBF16, 0, true);
-        if (c.axis == 0) PDELTA_GO(kBF16, 0, false);
-        if (grad) PDELTA_GO(kBF16, 1, true);
-        PDELTA_GO(kBF16, 1, false);
-    }
-    if (c.axis == 0 && grad) PDELTA_GO(kF16, 0, true);
-    if (c.axis == 0) PDELTA_GO(kF16, 0, false);
-    if (grad) PDELTA_GO(kF16, 1, true);
-    PDELTA_GO(kF16, 1, false);
+    auto tiles = [&]() {
+#define PDELTA_GO(WDT, AXIS, GRAD) return launch_big_tiles<WDT, AXIS, GRAD>(c, A, lda, inverse, partial, parts, stream)
+        if (c.dtype == kBF16) {
+            if (c.axis == 0 && grad) PDELTA_GO(kBF16, 0, true);
+            if (c.axis == 0) PDELTA_GO(kBF16, 0, false);
+            if (grad) PDELTA_GO(kBF16, 1, true);
+            PDELTA_GO(kBF16, 1, false);
+        }
+        if (c.axis == 0 && grad) PDELTA_GO(kF16, 0, true);
+        if (c.axis == 0) PDELTA_GO(kF16, 0, false);
+        if (grad) PDELTA_GO(kF16, 1, true);
+        PDELTA_GO(kF16, 1, false);
 #undef PDELTA_GO
+    };
+    if (const int rc = tiles(); rc != 0 || parts == 1) return rc;
+    const int64_t N = grad ? c.d_in : c.d_out, blocks = (N + 1023) / 1024;
+#define PDELTA_GO(YDT)                                                                                                              \
+    hipLaunchKernelGGL(experts_sum_kernel<YDT>, dim3((unsigned)(c.M * blocks)), dim3(256), 0, stream, partial, inverse, c.offsets, c.out, \
+                       (int)c.M, (int)c.E, (int)N, parts, (int)blocks)
+    if (c.out_dtype == kF32) PDELTA_GO(kF32);
+    else if (c.out_dtype == kBF16) PDELTA_GO(kBF16);
+    else PDELTA_GO(kF16);
+#undef PDELTA_GO
+    return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 }  // namespace pdelta

@@ -1,0 +1,83 @@
+// Forward product of tokens sorted by expert where an expert has few of them (decode of a mixture of experts): the decode tile of
+// the dense layer, 16 MT tokens of one expert x 16 NT output rows, for every expert that has tokens.  Memory-bound: the weights
+// of every expert that is met are read once for each 16 MT tokens of its, and those of the others not at all.
+//
+// A workgroup first looks its expert up, a load and a prefix sum away from its first weight, and ends with a sum over its waves;
+// two stages of a wave (or two row tiles and one) leave room for two workgroups on a CU, which cover each other's ends.
+#include <algorithm>
+
+#include "pdelta_experts.h"
+#include "pdelta_host.h"
+#include "pdelta_skinny_dma_tile.h"
+
+namespace pdelta {
+
+constexpr int expert_depth(int nt) { return nt == 1 ? 2 : 1; }
+
+template <int XDT, int AXIS, int MT, int NT>
+__global__ void __launch_bounds__(kDmaWaves * 64, 4)
+experts_skinny_kernel(const uint16_t* __restrict__ X, const int* __restrict__ offsets, const uint16_t* __restrict__ W_b, int64_t w_stride,
+                      const uint32_t* __restrict__ B_packed, const uint16_t* __restrict__ v, void* __restrict__ Y, int M, int E, int d_out,
+                      int d_in, int y_dtype, int row_tiles)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char dma_lds[];
+    ExpertTile t;
+    if (!find_expert_tile<MT * 16>(offsets, E, M, blockIdx.x / row_tiles, t)) return;       // whole workgroup
+    const int rows = min(t.end - t.row0, MT * 16);
+    char* out = (char*)Y + (int64_t)t.row0 * d_out * (y_dtype == kF32 ? 4 : 2);
+    linear_skinny_dma_tile<XDT, AXIS, MT, NT, expert_depth(NT)>(
+        X + (int64_t)t.row0 * d_in, W_b + t.expert * w_stride, B_packed + (int64_t)t.expert * d_out * (d_in / 32),
+        v + (int64_t)t.expert * (AXIS == 0 ? d_out : d_in), out, rows, d_out, d_in, y_dtype, 0, 0, blockIdx.x % row_tiles * (NT * 16), dma_lds);
+}
+
+template <int XDT, int AXIS, int MT, int NT>
+static int launch_skinny(const ExpertsCall& c, hipStream_t stream)
+{
+    constexpr int wave_lds = dma_wave_bytes(AXIS, MT, NT, expert_depth(NT)), lds = kDmaWaves * wave_lds;
+    static_assert(wave_lds >= MT * NT * 1024 && lds <= 160 * 1024, "LDS of a workgroup");
+    const int64_t row_tiles = (c.d_out + NT * 16 - 1) / (NT * 16), blocks = most_expert_tiles(c.M, c.E, MT * 16) * row_tiles;
+    if (blocks > 0x7FFFFFFF) return -2;
+    auto kernel = experts_skinny_kernel<XDT, AXIS, MT, NT>;
+    static unsigned lds_opted_in = 0;                 // per template instance: one kernel
+    if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kDmaWaves * 64), lds, stream, (const uint16_t*)c.tokens, c.offsets,
+                       (const uint16_t*)c.W_b, c.w_stride, c.B_packed, c.v, c.out, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype,
+                       (int)row_tiles);
+    return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+
+// Up to 16 tokens for each expert that can be met, always; up to 32 of bf16 (the tiles of 256 outputs convert their weights).
+// Uneven experts read their weights once for each 16 (32) of their tokens.  us here and on those tiles, experts x outputs x inputs,
+// bf16 row: 32 x 2048 x 4096, 10 tokens each 99 and 131, 24 120 and 140, 32 130 and 133; 8 x 4096 x 4096 10 43 and 64, 24 60 and 65;
+// 4 x 11008 x 4096 10 67 and 81, 24 96 and 83; fp16 col: 32 x 2048 x 4096 10 101 and 125, 24 137 and 128.
+int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
+{
+    (void)d_out;
+    if (M == 0 || d_in % kDmaUnitK != 0) return 0;
+    const int64_t met = std::min(E, M), each = (M + met - 1) / met;
+    const int forced = tune_value("experts_decode", -1);          // 0: never; 1 or 2
+    if (forced >= 0) return forced;
+    return each <= 16 ? 1 : each <= 32 && dtype == kBF16 ? 2 : 0;
+}
+
+int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream)
+{
+    // One row tile for a workgroup where it has a while to read (10 tokens for each of 32 experts, 2048 x 4096 bf16: 99 us, 120 with
+    // two), two for short rows (64 experts, 1408 x 2048: 82 and 70).
+    const bool one = c.d_in > 2048;
+#define PDELTA_GO(XDT, AXIS)                                              \
+    {                                                                     \
+        if (mt == 2) return launch_skinny<XDT, AXIS, 2, 2>(c, stream);    \
+        if (one) return launch_skinny<XDT, AXIS, 1, 1>(c, stream);        \
+        return launch_skinny<XDT, AXIS, 1, 2>(c, stream);                 \
+    }
+    if (c.dtype == kBF16) {
+        if (c.axis == 0) PDELTA_GO(kBF16, 0)
+        PDELTA_GO(kBF16, 1)
+    }
+    if (c.axis == 0) PDELTA_GO(kF16, 0)
+    PDELTA_GO(kF16, 1)
+#undef PDELTA_GO
+}
+
+}  // namespace pdelta

@@ -185,3 +185,23 @@ def test_a_captured_call_follows_the_offsets(dtype):
         for a, b in zip(got, calls()):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+# few tiles and a long contraction: cut into parts, whose sums are added by a second kernel; d_in and d_out of several hundred to thousands
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("counts,d_out,d_in", [([70], 96, 4096), ([3, 0, 100, 41], 300, 1408), ([1], 4100, 64), ([200, 90], 2050, 128), ([33] * 5, 999, 2944)])
+def test_long_contractions(counts, d_out, d_in, dtype, axis):
+    c = make(counts, d_out, d_in, dtype, axis, 300 + d_out, before=1, behind=2)
+    check_products(c, axis, dtype, f"{counts} {d_out}x{d_in} {dtype} axis {axis}")
+    check_products(c, axis, F32, f"{counts} {d_out}x{d_in} {dtype} axis {axis} fp32")
+    assert torch.equal(grad_x(c, axis, F32)[1:-2], grad_x(c, axis, F32)[1:-2])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("each", [1, 7, 16, 17, 30, 40])
+def test_every_number_of_tokens_of_decode(each, dtype):
+    """Experts with fewer and with more tokens than a call's average, on rows longer and shorter than one round of the waves."""
+    for d_in, axis in ((256, ROW), (1152, COL), (4096, ROW)):
+        c = make([0, each // 2, each, 2 * each, 0, each + 5], 56, d_in, dtype, axis, each, behind=1)
+        check_products(c, axis, dtype, f"{each} tokens {d_in} {dtype}")
