@@ -406,7 +406,7 @@ int pdelta_patch_group(const void* W_b, const uint32_t* B_packed, const uint16_t
  *   W_b       in   [E, d_out, d_in], or [d_out, d_in] with shared_base = 1
  *   B_packed  in   [E, d_out, d_in / 32] uint32
  *   v         in   FP16 [E, d_out] (axis PDELTA_ROW) or [E, d_in] (axis PDELTA_COL)
- *   E              1 .. 65536
+ *   E              1 .. 32768
  * Everything else is as for pdelta_linear_row: dense row-major matrices, 16-byte aligned pointers (offsets too), error codes,
  * no aliasing of outputs.  NaN and Inf in a token's row stay in that row's output.
  * workspace: at least ..._workspace_bytes of the call, which may be 0 (then NULL is fine); PDELTA_EWORKSPACE if it is missing

@@ -7,6 +7,7 @@ library has not been built, or a call is rejected, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -590,67 +591,84 @@ def pdelta_patch_group(W_b, B_packed, v, group: int, out=None):
 # offsets is int32 [E + 1] on the GPU: the tokens of expert e are the rows offsets[e] .. offsets[e + 1] - 1.
 # W_b is [E, d_out, d_in], or [d_out, d_in] shared by all experts; B_packed [E, d_out, d_in / 32]; v [E, d_out] or [E, d_in].
 
-def _on_this_device(**tensors):
-    """Kernels go to the current device's current stream: every tensor of the call has to be there."""
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
-            raise ValueError(f"{name} must be on the current GPU")
+def _here(t: torch.Tensor, name: str) -> int:
+    """The current device, whose current stream the kernels go to: the first tensor has to be there, and then the others."""
+    here = t.get_device()
+    if here < 0 or here != (_device() if _raw_stream is not None else torch.cuda.current_device()):
+        raise ValueError(f"{name} must be a tensor on the current GPU")
+    return here
 
 
-def _call_workspace(need: int, given: torch.Tensor | None):
-    """Workspace of a call that cannot do without: the caller's own, else one of this call's."""
-    if given is None and need > 0:
+def _at(t: torch.Tensor, here: int, name: str):
+    if t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on the current GPU")
+    return t.data_ptr() or None
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(name: str, *sizes) -> int:
+    """The library's answer for these sizes, on which alone it depends."""
+    return int(getattr(lib(), name)(*sizes))
+
+
+def _call_workspace(need: int, given: torch.Tensor | None, here: int):
+    """(address, bytes, tensor) of a call's workspace: the caller's own, else one of this call's."""
+    if given is None:
+        if need == 0:
+            return None, 0, None
         given = torch.empty(need, dtype=torch.uint8, device="cuda")
-    return given if given is not None and given.numel() > 0 else None
+    return _at(given, here, "workspace"), given.numel() * given.element_size(), given
 
 
-def _expert_delta(W_b, B_packed, v, axis: int, dtype):
+def _check_experts(W_b, B_packed, v, axis: int, dtype):
     """(experts, d_out, d_in, whether they share the base weights)"""
-    if axis not in (ROW, COL):
+    w, b, scales = W_b.shape, B_packed.shape, v.shape
+    if axis != ROW and axis != COL:
         raise ValueError("axis must be ROW or COL")
-    if W_b.dim() not in (2, 3) or B_packed.dim() != 3 or v.dim() != 2:
+    if len(w) not in (2, 3) or len(b) != 3 or len(scales) != 2:
         raise ValueError("W_b must be [E, d_out, d_in] or [d_out, d_in], B_packed [E, d_out, d_in / 32], v [E, d_out or d_in]")
-    E, (d_out, d_in) = B_packed.shape[0], W_b.shape[-2:]
-    if B_packed.shape[1] != d_out or B_packed.shape[2] * 32 != d_in or (W_b.dim() == 3 and W_b.shape[0] != E):
+    E, d_out, d_in = b[0], w[-2], w[-1]
+    if b[1] != d_out or b[2] * 32 != d_in or (len(w) == 3 and w[0] != E):
         raise ValueError("W_b and B_packed must agree in experts, d_out and d_in")
-    if v.shape[0] != E or v.shape[1] != (d_out if axis == ROW else d_in):
+    if scales[0] != E or scales[1] != (d_out if axis == ROW else d_in):
         raise ValueError("v must be [E, d_out] in row mode, [E, d_in] in column mode")
     if W_b.dtype != dtype or B_packed.dtype != torch.int32 or v.dtype != torch.float16:
         raise ValueError("W_b has the dtype of the tokens, B_packed is int32, v is float16")
-    return E, d_out, d_in, int(W_b.dim() == 2)
+    return E, d_out, d_in, int(len(w) == 2)
 
 
 def _check_offsets(offsets, E: int):
-    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] != E + 1:
+    if offsets.dtype != torch.int32 or offsets.shape != (E + 1,):
         raise ValueError("offsets must be int32 [E + 1]")
 
 
 def _expert_product(name: str, tokens, offsets, W_b, B_packed, v, axis: int, out, out_dtype, workspace, grad: bool):
-    if tokens.dim() != 2 or tokens.dtype not in (torch.float16, torch.bfloat16):
+    dtype, shape = tokens.dtype, tokens.shape
+    if len(shape) != 2 or (dtype != torch.float16 and dtype != torch.bfloat16):
         raise ValueError("the tokens must be a float16 or bfloat16 matrix")
-    E, d_out, d_in, shared = _expert_delta(W_b, B_packed, v, axis, tokens.dtype)
-    width_in, width_out = (d_out, d_in) if grad else (d_in, d_out)
-    M = tokens.shape[0]
-    if tokens.shape[1] != width_in:
+    E, d_out, d_in, shared = _check_experts(W_b, B_packed, v, axis, dtype)
+    M, width = shape[0], d_in if grad else d_out
+    if shape[1] != (d_out if grad else d_in):
         raise ValueError("the tokens and W_b must agree in " + ("d_out" if grad else "d_in"))
     if offsets is not None:
         _check_offsets(offsets, E)
+    here = _here(tokens, "the tokens")
     if out is None:
-        out = torch.empty((M, width_out), dtype=out_dtype or tokens.dtype, device=tokens.device)
-    elif out.shape != (M, width_out) or (out_dtype is not None and out.dtype != out_dtype):
+        out = torch.empty((M, width), dtype=out_dtype or dtype, device=tokens.device)
+    elif out.shape != (M, width) or (out_dtype is not None and out.dtype != out_dtype):
         raise ValueError("out must be one row of outputs for each token, of out_dtype")
-    _on_this_device(tokens=tokens, offsets=offsets, W_b=W_b, B_packed=B_packed, v=v, out=out, workspace=workspace)
-    L, dtype = lib(), _DTYPE_CODE[tokens.dtype]
-    need = getattr(L, f"pdelta_{'grad_x' if grad else 'linear'}_experts_workspace_bytes")(M, E, d_out, d_in, dtype)
-    ws = _call_workspace(need, workspace)
+    code, out_code = _DTYPE_CODE[dtype], dtype_code(out.dtype)
+    at = [_at(tokens, here, "the tokens"), _at(W_b, here, "W_b"), _at(B_packed, here, "B_packed"), _at(v, here, "v"), _at(out, here, "out")]
+    L = _lib if _lib is not None else lib()
     if offsets is None:
-        rc = L.pdelta_grad_x(_dev(tokens, "dY") or None, _dev(W_b, "W_b"), _dev(B_packed, "B_packed"), _dev(v, "v"), axis,
-                             _dev(out, "dX") or None, M, d_out, d_in, dtype, dtype_code(out.dtype), *_workspace_args(ws), _stream())
+        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_x_workspace_bytes", M, d_out, d_in, code), workspace, here)
+        rc = L.pdelta_grad_x(at[0], at[1], at[2], at[3], axis, at[4], M, d_out, d_in, code, out_code, ws, ws_bytes, _stream())
     else:
-        rc = getattr(L, name)(_dev(tokens, "tokens") or None, _dev(offsets, "offsets"), _dev(W_b, "W_b"), shared, _dev(B_packed, "B_packed"),
-                              _dev(v, "v"), axis, _dev(out, "out") or None, M, E, d_out, d_in, dtype, dtype_code(out.dtype),
-                              *_workspace_args(ws), _stream())
-    _check(rc, name)
+        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes(name + "_workspace_bytes", M, E, d_out, d_in, code), workspace, here)
+        rc = getattr(L, name)(at[0], _at(offsets, here, "offsets"), at[1], shared, at[2], at[3], axis, at[4], M, E, d_out, d_in, code, out_code,
+                              ws, ws_bytes, _stream())
+    if rc != OK:
+        raise PdeltaError(rc, name)
     return out
 
 
@@ -702,14 +720,14 @@ def pdelta_grad_v_experts(X, dY, offsets, B_packed, axis: int, out=None, workspa
         raise ValueError("B_packed must be int32 [E, d_out, d_in / 32]")
     E, kept = B_packed.shape[0], d_out if axis == ROW else d_in
     _check_offsets(offsets, E)
+    here = _here(X, "X")
     if out is None:
         out = torch.empty((E, kept), dtype=torch.float32, device=X.device)
     elif out.shape != (E, kept) or out.dtype != torch.float32:
         raise ValueError("out must be float32 [E, d_out] in row mode, [E, d_in] in column mode")
-    _on_this_device(X=X, dY=dY, offsets=offsets, B_packed=B_packed, out=out, workspace=workspace)
-    ws = _call_workspace(pdelta_grad_v_experts_workspace_bytes(M, E, d_out, d_in, axis), workspace)
-    rc = lib().pdelta_grad_v_experts(_dev(X, "X") or None, _dev(dY, "dY") or None, _dev(offsets, "offsets"), _dev(B_packed, "B_packed"),
-                                     axis, _dev(out, "grad_v"), M, E, d_out, d_in, dtype_code(X.dtype), *_workspace_args(ws), _stream())
+    at = [_at(X, here, "X"), _at(dY, here, "dY"), _at(offsets, here, "offsets"), _at(B_packed, here, "B_packed"), _at(out, here, "grad_v")]
+    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_v_experts_workspace_bytes", M, E, d_out, d_in, axis), workspace, here)
+    rc = lib().pdelta_grad_v_experts(at[0], at[1], at[2], at[3], axis, at[4], M, E, d_out, d_in, dtype_code(X.dtype), ws, ws_bytes, _stream())
     _check(rc, "pdelta_grad_v_experts")
     return out
 
@@ -736,15 +754,15 @@ def pdelta_distill(logits, top_ids, top_logits, weight=None, temperature: float 
         raise ValueError("weight must be float32 [T]")
     if out is not None and (not want_grad or out.shape != logits.shape or out.dtype != logits.dtype):
         raise ValueError("out is the gradient's buffer, like logits")
+    here, dtype = _here(logits, "logits"), dtype_code(logits.dtype)
     if want_grad and out is None:
-        out = torch.empty_like(logits)
+        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
     loss = torch.empty(T, dtype=torch.float32, device=logits.device)
-    _on_this_device(logits=logits, top_ids=top_ids, top_logits=top_logits, weight=weight, out=out, workspace=workspace)
-    ws = _call_workspace(pdelta_distill_workspace_bytes(T, V, k, logits.dtype), workspace)
-    rc = lib().pdelta_distill(_dev(logits, "logits") or None, _dev(top_ids, "top_ids") or None, _dev(top_logits, "top_logits") or None,
-                              _dev(weight, "weight") if weight is not None else None, _dev(loss, "loss") or None,
-                              (_dev(out, "grad") or None) if out is not None else None, T, V, k, dtype_code(logits.dtype),
-                              dtype_code(top_logits.dtype), temperature, grad_scale, *_workspace_args(ws), _stream())
+    at = [_at(logits, here, "logits"), _at(top_ids, here, "top_ids"), _at(top_logits, here, "top_logits"),
+          None if weight is None else _at(weight, here, "weight"), _at(loss, here, "loss"), None if out is None else _at(out, here, "out")]
+    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_distill_workspace_bytes", T, V, k, dtype), workspace, here)
+    rc = lib().pdelta_distill(at[0], at[1], at[2], at[3], at[4], at[5], T, V, k, dtype, dtype_code(top_logits.dtype), temperature, grad_scale,
+                              ws, ws_bytes, _stream())
     _check(rc, "pdelta_distill")
     return loss, out
 

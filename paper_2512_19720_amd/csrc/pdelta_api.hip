@@ -695,7 +695,7 @@ int pdelta_patch_group(const void* W_b, const uint32_t* B_packed, const uint16_t
 namespace pdelta {
 namespace {
 
-constexpr int64_t kMaxExperts = 1 << 16, kMaxWords = 1024;
+constexpr int64_t kMaxExperts = 1 << 15, kMaxWords = 1024;
 
 struct Buffer { const void* p; size_t bytes; };
 
@@ -728,7 +728,6 @@ int check_experts(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
 // Forward (grad = false: tokens X, out Y) and backward with respect to the input (tokens dY, out dX).
 int experts_product(const ExpertsCall& call, bool grad, bool dense, int shared_base, size_t workspace_bytes, void* stream)
 {
-    const TuneScope tune_scope;
     ExpertsCall c = call;
     if (c.W_b == nullptr || c.B_packed == nullptr || c.v == nullptr || (!dense && c.offsets == nullptr)) return PDELTA_EINVAL;
     if (shared_base != 0 && shared_base != 1) return PDELTA_EINVAL;
@@ -763,7 +762,6 @@ static bool experts_sizes_ok(int64_t M, int64_t E, int64_t d_out, int64_t d_in, 
 
 size_t pdelta_linear_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype)
 {
-    const pdelta::TuneScope tune_scope;
     if (!experts_sizes_ok(M, E, d_out, d_in, PDELTA_ROW) || !pdelta::is_w_dtype(x_dtype)) return 0;
     return pdelta::experts_linear_workspace_bytes(M, E, d_out, d_in, x_dtype);
 }
@@ -778,7 +776,6 @@ int pdelta_linear_experts(const void* X, const int32_t* offsets, const void* W_b
 
 size_t pdelta_grad_x_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
 {
-    const pdelta::TuneScope tune_scope;
     if (!experts_sizes_ok(M, E, d_out, d_in, PDELTA_ROW) || !pdelta::is_w_dtype(dtype)) return 0;
     return pdelta::experts_grad_x_workspace_bytes(M, E, d_out, d_in, dtype);
 }
@@ -805,7 +802,6 @@ int pdelta_grad_x(const void* dY, const void* W_b, const uint32_t* B_packed, con
 
 size_t pdelta_grad_v_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
 {
-    const pdelta::TuneScope tune_scope;
     if (!experts_sizes_ok(M, E, d_out, d_in, axis)) return 0;
     return pdelta::experts_grad_v_workspace_bytes(M, E, d_out, d_in, axis);
 }
@@ -815,7 +811,6 @@ int pdelta_grad_v_experts(const void* X, const void* dY, const int32_t* offsets,
                           void* stream)
 {
     using namespace pdelta;
-    const TuneScope tune_scope;
     if (offsets == nullptr || B_packed == nullptr || grad_v == nullptr) return PDELTA_EINVAL;
     if (const int rc = check_experts(M, E, d_out, d_in, axis)) return rc;
     if (M > 0 && (X == nullptr || dY == nullptr)) return PDELTA_EINVAL;
@@ -841,7 +836,6 @@ static int distill_sizes(int64_t T, int64_t V, int64_t k)
 
 size_t pdelta_distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype)
 {
-    const pdelta::TuneScope tune_scope;
     if (distill_sizes(T, V, k) != PDELTA_OK || !pdelta::is_y_dtype(dtype)) return 0;
     return pdelta::distill_workspace_bytes(T, V, k, dtype);
 }
@@ -851,7 +845,6 @@ int pdelta_distill(const void* logits, const int32_t* top_ids, const void* top_l
                    void* workspace, size_t workspace_bytes, void* stream)
 {
     using namespace pdelta;
-    const TuneScope tune_scope;
     if (const int rc = distill_sizes(T, V, k)) return rc;
     if (T > 0 && (logits == nullptr || top_ids == nullptr || top_logits == nullptr || loss == nullptr)) return PDELTA_EINVAL;
     if (!(temperature >= 1e-6f && temperature <= 1e6f) || !std::isfinite(grad_scale)) return PDELTA_EINVAL;

@@ -4,7 +4,8 @@
 // W_b that it has itself loaded into W_hat in place, between its matrix instructions; one barrier per step, three quarters into
 // it, which publishes step s + 1 and frees the stage of step s for step s + 2.
 //
-// The tokens come as fp16 rows of a multiple of 128 values (prepared ones, or X and dY themselves).
+// The tokens come as fp16 rows of a multiple of 128 values (prepared ones, or X and dY themselves); forward, the signs as rows of a
+// multiple of 16 bytes.
 //
 // Forward: a tile of W_hat is 256 output rows x 64 inputs; both operands' fragments are 16 consecutive bytes of a row.
 // GRAD: it is 64 output rows x 256 inputs, as it lies in memory, and the contraction runs over the rows: fragments are read by
@@ -39,7 +40,7 @@ struct TileArgs {
     const uint16_t* v;
     void* Y;
     float* partial;
-    int M, d_out, d_in, y_dtype, parts;
+    int M, d_out, d_in, y_dtype, parts, sign_ld;      // sign_ld: bytes from one output row's signs to the next
 };
 
 // One tile of 64 FM tokens, waves of 32 FM x 64 outputs.
@@ -65,7 +66,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     const int first_step = (int)((int64_t)(lda / kTileK / 2) * part / g.parts) * 2;
     const int n_steps = (int)((int64_t)(lda / kTileK / 2) * (part + 1) / g.parts) * 2 - first_step;
     const uint16_t* W = g.W_b + t.expert * g.w_stride;
-    const uint32_t* B = g.B_packed + (int64_t)t.expert * d_out * (d_in / 32);
+    const char* B = (const char*)g.B_packed + (int64_t)t.expert * d_out * g.sign_ld;
     const uint16_t* scales = v + (int64_t)t.expert * (AXIS == 0 ? d_out : d_in);
 
     const int lane = threadIdx.x & 63;
@@ -93,7 +94,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     uint4v vcol[2];                                   // GRAD column mode: the scales of the lane's inputs
     if constexpr (GRAD) {
         wbase = (const char*)W;
-        sbase = (const char*)B;
+        sbase = B;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             chunk[q] = (uint32_t)((lane & 31) ^ ((q * 2 + (lane >> 5)) << 2));
@@ -104,24 +105,24 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
         soff = (uint32_t)min(n0 / 32 + (lane & 7), d_in / 32 - 1) * 4u;
     } else {
         wbase = (const char*)(W + (int64_t)n0 * d_in);
-        sbase = (const char*)B + (int64_t)n0 * (d_in >> 3);
+        sbase = B + (int64_t)n0 * g.sign_ld;
 #pragma unroll
         for (int q = 0; q < 2; ++q) chunk[q] = piece[q];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int row = min(n0 + wave * 32 + q * 8 + (lane >> 3), d_out - 1) - n0;
-            woff[q] = (uint32_t)row * (uint32_t)d_in * 2u + chunk[q & 1] * 16u;
+            woff[q] = (uint32_t)row * (uint32_t)d_in * 2u;
             if constexpr (AXIS == 0) vrow[q] = (uint32_t)scales[n0 + row] * 0x10001u;
         }
         // lanes 0-31: sign words of the wave's rows for two steps, lanes 32-63 for the next two
-        soff = (uint32_t)(min(n0 + wave * 32 + (lane & 31), d_out - 1) - n0) * (uint32_t)(d_in >> 3);
+        soff = (uint32_t)(min(n0 + wave * 32 + (lane & 31), d_out - 1) - n0) * (uint32_t)g.sign_ld;
     }
 
     // Where step s is in the contraction.  Forward, with one token tile: the output tiles start at different places of d_in, since rows
     // of W_b are often a power of two apart and the same inputs of all rows then in few of the memory's channels (16 experts of 64
-    // tokens, 4096 x 4096 fp16: 138 -> 117 us).  With more of them the tokens are better read by all at once (2048 tokens of one
-    // expert, 8192 x 4096: 131 and 135).
-    const int start = GRAD || t.tiles > 1 ? 0 : (tile_n + (g.w_stride != 0 ? t.expert * 5 : 0)) * 6 % n_steps / 2 * 2;
+    // tokens, 4096 x 4096 fp16: 138 -> 117 us).  With more of them, or one base for all experts, the weights or tokens that workgroups
+    // share are better read by all at once (2048 tokens of one expert, 8192 x 4096: 131 and 135; 1501 of 12 fine-tunes: 118 and 122).
+    const int start = GRAD || t.tiles > 1 || g.w_stride == 0 ? 0 : (tile_n + t.expert * 5) * 6 % n_steps / 2 * 2;
     auto place = [&](int s) {
         if constexpr (GRAD) return first_step + s;
         s += start;
@@ -133,14 +134,14 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
         if constexpr (GRAD) {
             const int kb = place(s) * kTileK, k0 = min(kb, d_out - 1);        // rows behind the last one repeat it: the tokens are zero there
             auto row = [&](int r) { return (uint32_t)(min(kb + r, d_out - 1) - k0); };
-            load_lds_4(my_signs + (s & 3) * 256, row(wave * 8 + (lane >> 3)) * (uint32_t)(d_in >> 3) + soff, sbase + (int64_t)k0 * (d_in >> 3));
+            load_lds_4(my_signs + (s & 3) * 256, row(wave * 8 + (lane >> 3)) * (uint32_t)g.sign_ld + soff, sbase + (int64_t)k0 * g.sign_ld);
             if constexpr (AXIS == 0)
                 if (lane < 8) load_lds_2(my_scales + (s & 3) * 32, row(wave * 8 + lane) * 2u, scales + k0);
         } else {
             const int group = (s >> 2) & 1;
             load_lds_16(my_signs + group * 1024, soff + (uint32_t)place(min(s + (lane >> 5) * 2, n_steps - 2)) * 8u, sbase);
             if constexpr (AXIS == 1)
-                if (lane < 32) load_lds_16(my_scales + group * 512, (uint32_t)(place(min(s + (lane >> 3), n_steps - 1)) * 64 + (lane & 7) * 8) * 2u, scales);
+                if (lane < 32) load_lds_16(my_scales + group * 512, (uint32_t)min(place(min(s + (lane >> 3), n_steps - 1)) * 64 + (lane & 7) * 8, d_in - 8) * 2u, scales);
         }
     };
     auto request_a = [&](int s, uint32_t stage) {
@@ -159,9 +160,12 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             for (int q = 0; q < 4; ++q)
                 into[q] = *(const uint4v*)(base + ((uint32_t)(min(kb + wave * 8 + q * 2 + (lane >> 5), d_out - 1) - k0) * (uint32_t)d_in * 2u + woff[q & 1]));
         } else {
-            const char* base = wbase + (int64_t)place(s) * (kTileK * 2);
+            const int kb = place(s) * kTileK;             // inputs behind the last ones repeat them: the tokens are zero there
+            uint32_t col[2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) into[q] = *(const uint4v*)(base + woff[q]);
+            for (int q = 0; q < 2; ++q) col[q] = (uint32_t)min(kb + (int)chunk[q] * 8, d_in - 8) * 2u;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) into[q] = *(const uint4v*)(wbase + (woff[q] + col[q & 1]));
         }
     };
 
@@ -407,10 +411,10 @@ __global__ void __launch_bounds__(512, 2)
 experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
                    const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
                    const uint16_t* __restrict__ v, void* __restrict__ Y, float* __restrict__ partial, int M, int E, int d_out, int d_in, int y_dtype,
-                   int n_tiles, int parts)
+                   int n_tiles, int parts, int sign_ld)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
-    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts};
+    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts, sign_ld};
     ExpertTile t;
     int tile_n;
     {
@@ -469,7 +473,8 @@ int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K)
 }
 
 template <int WDT, int AXIS, bool GRAD>
-static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, float* partial, int parts, hipStream_t stream)
+static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, float* partial, int parts, int sign_ld,
+                            hipStream_t stream)
 {
     constexpr int lds = kTileLds;
     const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
@@ -479,15 +484,15 @@ static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, co
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), lds, stream, A, lda, inverse, c.offsets, (const uint16_t*)c.W_b, c.w_stride,
-                       c.B_packed, c.v, c.out, partial, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles, parts);
+                       c.B_packed, c.v, c.out, partial, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles, parts, sign_ld);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, float* partial, int parts,
-                       hipStream_t stream)
+                       int sign_ld, hipStream_t stream)
 {
     auto tiles = [&]() {
-#define PDELTA_GO(WDT, AXIS, GRAD) return launch_big_tiles<WDT, AXIS, GRAD>(c, A, lda, inverse, partial, parts, stream)
+#define PDELTA_GO(WDT, AXIS, GRAD) return launch_big_tiles<WDT, AXIS, GRAD>(c, A, lda, inverse, partial, parts, sign_ld, stream)
         if (c.dtype == kBF16) {
             if (c.axis == 0 && grad) PDELTA_GO(kBF16, 0, true);
             if (c.axis == 0) PDELTA_GO(kBF16, 0, false);

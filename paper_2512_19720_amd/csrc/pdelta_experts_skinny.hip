@@ -50,13 +50,10 @@ static int launch_skinny(const ExpertsCall& c, hipStream_t stream)
 // Uneven experts read their weights once for each 16 (32) of their tokens.  us here and on those tiles, experts x outputs x inputs,
 // bf16 row: 32 x 2048 x 4096, 10 tokens each 99 and 131, 24 120 and 140, 32 130 and 133; 8 x 4096 x 4096 10 43 and 64, 24 60 and 65;
 // 4 x 11008 x 4096 10 67 and 81, 24 96 and 83; fp16 col: 32 x 2048 x 4096 10 101 and 125, 24 137 and 128.
-int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
+int experts_decode_tokens(int64_t M, int64_t E, int64_t d_in, int dtype)
 {
-    (void)d_out;
     if (M == 0 || d_in % kDmaUnitK != 0) return 0;
     const int64_t met = std::min(E, M), each = (M + met - 1) / met;
-    const int forced = tune_value("experts_decode", -1);          // 0: never; 1 or 2
-    if (forced >= 0) return forced;
     return each <= 16 ? 1 : each <= 32 && dtype == kBF16 ? 2 : 0;
 }
 

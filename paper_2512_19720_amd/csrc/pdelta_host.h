@@ -155,15 +155,15 @@ int launch_experts_linear(const ExpertsCall& c, hipStream_t stream);
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream);
 
 // The forward product where experts have few tokens, 16 mt at a time.  experts_decode_tokens: that mt, or 0 for the tiles below.
-int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype);
+int experts_decode_tokens(int64_t M, int64_t E, int64_t d_in, int dtype);
 int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream);
 
 // The products on tiles of 256 outputs with direct loads: A holds fp16 rows of lda values, a multiple of 128; inverse: a factor for
 // each row of the outputs, or NULL; partial: parts x M x (outputs) fp32 where the contraction, K long, is cut into more than one
-// part.  Forward: d_in a multiple of 128.
+// part; sign_ld: bytes between the signs of two output rows (c.B_packed), forward a multiple of 16.
 int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K);
 int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, float* partial, int parts,
-                       hipStream_t stream);
+                       int sign_ld, hipStream_t stream);
 
 // Rows of K 16-bit values copied into rows of experts_padded(K), zeros behind them.
 constexpr int64_t experts_padded(int64_t K) { return (K + 127) / 128 * 128; }

@@ -35,7 +35,7 @@ def test_product_refusals(fn):
     assert product(fn, M=0) == pd.OK and product(fn, M=0, tok=None, out=None, ws=None, ws_bytes=0) == pd.OK
 
 
-@pytest.mark.parametrize("fn,sizes", [("pdelta_linear_experts", (100, 4, 96, 128, pd.BF16)), ("pdelta_grad_x_experts", (100, 4, 96, 128, pd.BF16)),
+@pytest.mark.parametrize("fn,sizes", [("pdelta_linear_experts", (1000, 4, 96, 128, pd.BF16)), ("pdelta_grad_x_experts", (100, 4, 96, 128, pd.BF16)),
                                       ("pdelta_grad_x_experts", (100, 4, 97, 128, pd.F16))])
 def test_product_workspace(fn, sizes):
     M, E, d_out, d_in, dt = sizes
@@ -45,6 +45,7 @@ def test_product_workspace(fn, sizes):
     assert product(fn, ws_bytes=need - 1, **args) == pd.EWORKSPACE
     assert product(fn, ws=None, ws_bytes=0, **args) == pd.EWORKSPACE
     assert product(fn, ws=None, ws_bytes=need, **args) == pd.EINVAL
+    assert getattr(pd.lib(), fn + "_workspace_bytes")(0, *sizes[1:]) == 0
     for bad in ((-1, 4, 96, 128, dt), (100, 0, 96, 128, dt), (100, 4, 0, 128, dt), (100, 4, 96, 100, dt), (100, 4, 96, 128, pd.F32)):
         assert getattr(pd.lib(), fn + "_workspace_bytes")(*bad) == 0
 
