@@ -10,7 +10,7 @@
 // the teacher's words meanwhile.  The gradient is written as if the teacher had named no word, and the words' own entries again
 // after a barrier.
 //
-// With fewer tokens than CUs a row is split among workgroups: one launch leaves every part's largest logit and sum (and the
+// Of few tokens, a long row is split among workgroups: one launch leaves every part's largest logit and sum (and the
 // words' logits, since the gradient may replace the logits) in the workspace, a second one joins them in their order.
 #include <algorithm>
 #include <cmath>
@@ -312,6 +312,8 @@ distill_kernel(DistillArgs g)
     store_words<DT>(g, row, words, q_factor, factor, all.most, 0, g.V);
 }
 
+constexpr int kPartVectors = 8;                       // of a thread: 32 KB for a workgroup
+
 // Words of part `part` of a row that is split into g.parts: multiples of 64 words.
 __device__ __forceinline__ void part_of(const DistillArgs& g, int part, int64_t& begin, int64_t& end)
 {
@@ -321,7 +323,7 @@ __device__ __forceinline__ void part_of(const DistillArgs& g, int part, int64_t&
 }
 
 // Split rows: largest logit and sum of one part, and the logits of the teacher's words in it.
-template <int DT, int NV>
+template <int DT>
 __global__ void __launch_bounds__(256)
 distill_part_kernel(DistillArgs g)
 {
@@ -331,7 +333,7 @@ distill_part_kernel(DistillArgs g)
     int64_t begin, end;
     part_of(g, part, begin, end);
     if (g.weight != nullptr && g.weight[row] == 0.f) return;      // whole workgroup
-    RowPart<DT, 256, NV> p;
+    RowPart<DT, 256, kPartVectors> p;
     p.load(g.logits, nullptr, row, g.V, begin, end);
     for (int j = threadIdx.x; j < g.k; j += 256) {
         const int id = g.ids[row * g.k + j];
@@ -351,7 +353,7 @@ distill_part_kernel(DistillArgs g)
 }
 
 // Split rows: the parts' sums together; the loss (from the first part's workgroup) and the part's gradient.
-template <int DT, int NV>
+template <int DT>
 __global__ void __launch_bounds__(256)
 distill_join_kernel(DistillArgs g, int groups)
 {
@@ -370,7 +372,7 @@ distill_join_kernel(DistillArgs g, int groups)
         }
         return;
     }
-    RowPart<DT, 256, NV> p;
+    RowPart<DT, 256, kPartVectors> p;
     if (g.grad != nullptr) p.load(g.logits, g.grad, row, g.V, begin, end);
     Sum all{kNothing, 0.f};
     for (int k = 0; k < g.parts; ++k) all = join(all, g.sums[row * g.parts + k], g.tau);
@@ -387,19 +389,19 @@ distill_join_kernel(DistillArgs g, int groups)
     store_words<DT>(g, row, words, q_factor, factor, all.most, begin, end);
 }
 
-// Parts of a row: with fewer tokens than CUs as many as give every CU two workgroups, of 2048 words at least.
-static int row_parts(int64_t T, int64_t V)
+// Parts of a row: of few tokens, rows of more than 128 KB are split into parts of 32 KB.  us in one part, 4, 8 and 16: 1 x 128256 bf16
+// 18.5, 16.0, 11.7 and 12.4, 64 tokens 21.1, 19.6, 15.7 and 19.0, 150 tokens 24.3, 30.3, 26.3 and 33.7; 16 x 128256 fp32 24.0, 23.5, 16.2
+// and 12.9; but 3 x 32001 fp32 (125 KB) 9.2, 10.6, 10.8 and 10.7.
+static int row_parts(int64_t T, int64_t V, int dtype)
 {
-    if (T >= 256) return 1;
-    const int64_t most = (V + 2047) / 2048, want = 512 / T;
-    return (int)std::max<int64_t>(1, std::min(most, want));
+    const int64_t bytes = V * (dtype == kF32 ? 4 : 2);
+    return T > 128 || bytes <= 128 * 1024 ? 1 : (int)std::min<int64_t>(32, bytes / (32 * 1024));
 }
 
 size_t distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype)
 {
-    (void)dtype;
     if (T == 0) return 0;
-    const int parts = row_parts(T, V);
+    const int parts = row_parts(T, V, dtype);
     return parts == 1 ? 0 : (size_t)T * ((size_t)parts * sizeof(Sum) + (size_t)k * 4);
 }
 
@@ -414,20 +416,13 @@ static int launch_rows(const DistillCall& c, hipStream_t stream)
     tau.lo = (float)(factor - (double)tau.hi);
     tau.tau = c.temperature;
     DistillArgs g{c.logits, c.ids, c.top, c.weight, c.loss, c.grad, c.V, (int)c.k, c.top_dtype, tau, c.grad_scale, nullptr, nullptr, 1};
-    g.parts = row_parts(c.T, c.V);
+    g.parts = row_parts(c.T, c.V, c.dtype);
     if (g.parts > 1) {
         g.sums = (Sum*)c.workspace;
         g.words_z = (float*)(g.sums + c.T * g.parts);
         const int groups = c.grad != nullptr ? g.parts : 1;
-        const int64_t vectors = ((c.V + 63) / 64 + g.parts - 1) / g.parts * 64 / PER;
-#define PDELTA_GO(NV)                                                                                                              \
-        {                                                                                                                          \
-            hipLaunchKernelGGL((distill_part_kernel<DT, NV>), dim3((unsigned)(c.T * g.parts)), dim3(256), 0, stream, g);           \
-            hipLaunchKernelGGL((distill_join_kernel<DT, NV>), dim3((unsigned)(c.T * groups)), dim3(256), 0, stream, g, groups);    \
-        }
-        if (vectors <= 2 * 256) PDELTA_GO(2)
-        else PDELTA_GO(8)
-#undef PDELTA_GO
+        hipLaunchKernelGGL(distill_part_kernel<DT>, dim3((unsigned)(c.T * g.parts)), dim3(256), 0, stream, g);
+        hipLaunchKernelGGL(distill_join_kernel<DT>, dim3((unsigned)(c.T * groups)), dim3(256), 0, stream, g, groups);
     } else {
         const int64_t vectors = c.V / PER;
 #define PDELTA_GO(THREADS, NV) hipLaunchKernelGGL((distill_kernel<DT, THREADS, NV>), dim3((unsigned)c.T), dim3(THREADS), 0, stream, g)

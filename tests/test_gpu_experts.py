@@ -205,3 +205,14 @@ def test_every_number_of_tokens_of_decode(each, dtype):
     for d_in, axis in ((256, ROW), (1152, COL), (4096, ROW)):
         c = make([0, each // 2, each, 2 * each, 0, each + 5], 56, d_in, dtype, axis, each, behind=1)
         check_products(c, axis, dtype, f"{each} tokens {d_in} {dtype}")
+
+
+@pytest.mark.parametrize("axis", [ROW, COL])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("counts,d_out,d_in", [([9, 0, 70, 1], 2600, 2080), ([40] * 9, 1300, 1056), ([200, 3], 1032, 4128)])
+def test_grad_v_in_runs(counts, d_out, d_in, dtype, axis):
+    """Several tiles of the summed dimension for a workgroup, the last of them a short one; experts of one step and of several."""
+    c = make(counts, d_out, d_in, dtype, axis, 400 + d_out, before=3, behind=1)
+    got = pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis)
+    held(got, *grad_v64(c["X"], c["dY"], c["offsets"], c["B"], axis), f"grad_v {counts} {d_out}x{d_in} {dtype} axis {axis}")
+    assert torch.equal(got, pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis))
