@@ -611,12 +611,12 @@ def _workspace_bytes(name: str, *sizes) -> int:
     return int(getattr(lib(), name)(*sizes))
 
 
-def _call_workspace(need: int, given: torch.Tensor | None, here: int):
-    """(address, bytes, tensor) of a call's workspace: the caller's own, else one of this call's."""
+def _call_workspace(need: int, given: torch.Tensor | None, here: int, tensor: torch.Tensor):
+    """(address, bytes, tensor) of a call's workspace: the caller's own, else one of this call's, where `tensor` is."""
     if given is None:
         if need == 0:
             return None, 0, None
-        given = torch.empty(need, dtype=torch.uint8, device="cuda")
+        given = tensor.new_empty(need, dtype=torch.uint8)
     return _at(given, here, "workspace"), given.numel() * given.element_size(), given
 
 
@@ -661,10 +661,10 @@ def _expert_product(name: str, tokens, offsets, W_b, B_packed, v, axis: int, out
     at = [_at(tokens, here, "the tokens"), _at(W_b, here, "W_b"), _at(B_packed, here, "B_packed"), _at(v, here, "v"), _at(out, here, "out")]
     L = _lib if _lib is not None else lib()
     if offsets is None:
-        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_x_workspace_bytes", M, d_out, d_in, code), workspace, here)
+        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_x_workspace_bytes", M, d_out, d_in, code), workspace, here, tokens)
         rc = L.pdelta_grad_x(at[0], at[1], at[2], at[3], axis, at[4], M, d_out, d_in, code, out_code, ws, ws_bytes, _stream())
     else:
-        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes(name + "_workspace_bytes", M, E, d_out, d_in, code), workspace, here)
+        ws, ws_bytes, _keep = _call_workspace(_workspace_bytes(name + "_workspace_bytes", M, E, d_out, d_in, code), workspace, here, tokens)
         rc = getattr(L, name)(at[0], _at(offsets, here, "offsets"), at[1], shared, at[2], at[3], axis, at[4], M, E, d_out, d_in, code, out_code,
                               ws, ws_bytes, _stream())
     if rc != OK:
@@ -722,11 +722,11 @@ def pdelta_grad_v_experts(X, dY, offsets, B_packed, axis: int, out=None, workspa
     _check_offsets(offsets, E)
     here = _here(X, "X")
     if out is None:
-        out = torch.empty((E, kept), dtype=torch.float32, device=X.device)
+        out = X.new_empty((E, kept), dtype=torch.float32)
     elif out.shape != (E, kept) or out.dtype != torch.float32:
         raise ValueError("out must be float32 [E, d_out] in row mode, [E, d_in] in column mode")
     at = [_at(X, here, "X"), _at(dY, here, "dY"), _at(offsets, here, "offsets"), _at(B_packed, here, "B_packed"), _at(out, here, "grad_v")]
-    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_v_experts_workspace_bytes", M, E, d_out, d_in, axis), workspace, here)
+    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_grad_v_experts_workspace_bytes", M, E, d_out, d_in, axis), workspace, here, X)
     rc = lib().pdelta_grad_v_experts(at[0], at[1], at[2], at[3], axis, at[4], M, E, d_out, d_in, dtype_code(X.dtype), ws, ws_bytes, _stream())
     _check(rc, "pdelta_grad_v_experts")
     return out
@@ -756,11 +756,11 @@ def pdelta_distill(logits, top_ids, top_logits, weight=None, temperature: float 
         raise ValueError("out is the gradient's buffer, like logits")
     here, dtype = _here(logits, "logits"), dtype_code(logits.dtype)
     if want_grad and out is None:
-        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
-    loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+        out = torch.empty_like(logits)
+    loss = logits.new_empty(T, dtype=torch.float32)
     at = [_at(logits, here, "logits"), _at(top_ids, here, "top_ids"), _at(top_logits, here, "top_logits"),
           None if weight is None else _at(weight, here, "weight"), _at(loss, here, "loss"), None if out is None else _at(out, here, "out")]
-    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_distill_workspace_bytes", T, V, k, dtype), workspace, here)
+    ws, ws_bytes, _keep = _call_workspace(_workspace_bytes("pdelta_distill_workspace_bytes", T, V, k, dtype), workspace, here, logits)
     rc = lib().pdelta_distill(at[0], at[1], at[2], at[3], at[4], at[5], T, V, k, dtype, dtype_code(top_logits.dtype), temperature, grad_scale,
                               ws, ws_bytes, _stream())
     _check(rc, "pdelta_distill")

@@ -42,8 +42,12 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
     const int kt = blockIdx.x % kept_tiles, rt = blockIdx.x / kept_tiles % runs, e = blockIdx.x / kept_tiles / runs;
     int first, end;
     expert_rows(offsets, e, M, first, end);
-    if (first == end) return;                         // whole workgroup
     const int dP = AXIS == 0 ? d_in : d_out, dQ = AXIS == 0 ? d_out : d_in;
+    if (first == end) {                               // whole workgroup
+        const int q = kt * kGradTile + threadIdx.x;   // one run: these are the gradients
+        if (runs == 1 && threadIdx.x < kGradTile && q < dQ) partial[(int64_t)e * dQ + q] = 0.f;
+        return;
+    }
     const int p_ld = AXIS == 0 ? x_ld : y_ld, q_ld = AXIS == 0 ? y_ld : x_ld;
     const int q0 = kt * kGradTile, words = d_in / 32, first_tile = rt * run, tiles = min(run, sum_tiles - first_tile);
     const int lane = threadIdx.x & 63;
@@ -281,7 +285,8 @@ static int64_t grad_runs(int64_t M, int64_t E, int64_t kept, int64_t summed)
 // dY with rows that are no multiple of 16 bytes is copied into rows that are, behind the runs' sums.
 static int64_t sums_bytes(int64_t M, int64_t E, int64_t kept, int64_t summed)
 {
-    return (E * grad_runs(M, E, kept, summed) * kept * 4 + 15) / 16 * 16;
+    const int64_t runs = grad_runs(M, E, kept, summed);
+    return runs == 1 ? 0 : (E * runs * kept * 4 + 15) / 16 * 16;
 }
 
 size_t experts_grad_v_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int axis)
@@ -303,6 +308,7 @@ static int launch_grad(const void* X, const void* dY, const int* offsets, const 
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, kGradLds, &lds_opted_in) != 0) return -1;
     int64_t y_ld = d_out;
+    float* sums = runs == 1 ? grad : (float*)workspace;
     if (M > 0) {
         if ((d_out & 7) != 0) {
             void* rows = (char*)workspace + sums_bytes(M, E, kept, summed);
@@ -311,11 +317,12 @@ static int launch_grad(const void* X, const void* dY, const int* offsets, const 
             dY = rows;
         }
         hipLaunchKernelGGL(kernel, dim3((unsigned)(E * kept_tiles * runs)), dim3(512), kGradLds, stream, (const uint16_t*)X, (int)d_in,
-                           (const uint16_t*)dY, (int)y_ld, offsets, B_packed, (float*)workspace, (int)M, (int)d_out, (int)d_in,
+                           (const uint16_t*)dY, (int)y_ld, offsets, B_packed, sums, (int)M, (int)d_out, (int)d_in,
                            (int)kept_tiles, (int)sum_tiles, tiles_in_a_run(M, E, kept, summed), (int)runs);
     }
-    hipLaunchKernelGGL(experts_grad_sum_kernel, dim3((unsigned)(E * sum_blocks)), dim3(256), 0, stream, (const float*)workspace, offsets,
-                       grad, (int)M, (int)kept, (int)runs, (int)sum_blocks);
+    if (M == 0 || runs > 1)
+        hipLaunchKernelGGL(experts_grad_sum_kernel, dim3((unsigned)(E * sum_blocks)), dim3(256), 0, stream, (const float*)workspace, offsets,
+                           grad, (int)M, (int)kept, (int)runs, (int)sum_blocks);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
