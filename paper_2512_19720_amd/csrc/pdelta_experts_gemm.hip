@@ -107,7 +107,7 @@ struct ProductLayout {
         factors = prepare ? (size_t)(M * experts_padded(K)) * 2 : 0;
         signs = factors + (prepare ? (size_t)(M + 3) / 4 * 16 : 0);
         partial = signs + (wide_signs ? (size_t)(E * d_out * experts_padded(d_in) / 8) : 0);
-        all = partial + (parts > 1 ? (size_t)(parts * M * N) * 4 : 0);
+        all = partial + (parts > 1 ? (size_t)(parts * M * experts_pitch(N)) * 4 : 0);
     }
 };
 

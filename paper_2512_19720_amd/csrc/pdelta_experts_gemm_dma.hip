@@ -30,6 +30,32 @@ constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
 // four steps), and its scales (1 KB: forward column mode, v for two groups of four steps; GRAD row mode, its 8 rows' for four)
 constexpr int kTileW = 2 * kTileM * kTileK * 2, kTileSigns = kTileW + 2 * kWBytes, kTileScales = kTileSigns + 8 * 2048, kTileLds = kTileScales + 8 * 1024;
 
+// The wave tile's outputs one by one, columns in 128-byte pieces of a row: 16-bit outputs whose rows are no multiple of 16 bytes, fp32
+// ones and the parts' sums (rows `pitch` apart).  A row's address is scalar, the lane's place in it one register; rows behind
+// `end` and columns behind N are left out.
+template <int YDT, int FM>
+__device__ __forceinline__ void store_rows(const float16v (&acc)[FM][2], void* Y, int64_t pitch, int m0, int n0, int end, int N, int lane)
+{
+    constexpr int SIZE = YDT == kF32 ? 4 : 2;
+    const int low = (lane >> 5) * 4;
+    const uint32_t at = (uint32_t)((int64_t)low * pitch + (lane & 31)) * (uint32_t)SIZE;          // pitch <= 2^22 + 255
+#pragma unroll
+    for (int f = 0; f < FM; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = m0 + f * 32 + (r >> 2) * 8 + (r & 3);
+            char* const base = (char*)Y + ((int64_t)row * pitch + n0) * SIZE;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (row + low < end && n0 + h * 32 + (lane & 31) < N) {
+                    const float x = acc[f][h][r];
+                    char* const p = base + h * 32 * SIZE + at;
+                    if constexpr (YDT == kF32) *(float*)p = x;
+                    else *(uint16_t*)p = (uint16_t)(YDT == kBF16 ? f32_to_bf16_bits(x) : f32_to_f16_bits(x));
+                }
+        }
+}
+
 struct TileArgs {
     const uint16_t* A;
     int lda;
@@ -40,7 +66,7 @@ struct TileArgs {
     const uint16_t* v;
     void* Y;
     float* partial;
-    int M, d_out, d_in, y_dtype, parts, sign_ld;      // sign_ld: bytes from one output row's signs to the next
+    int M, d_out, d_in, y_dtype, parts, sign_ld, pitch;     // bytes from one output row's signs to the next; values of a row of the parts' sums
 };
 
 // One tile of 64 FM tokens, waves of 32 FM x 64 outputs.
@@ -59,7 +85,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     // (a part leaves its sums as they are; experts_sum_kernel does the rest)
     const float* inverse = g.parts > 1 ? nullptr : g.inverse;
     const int lda = g.lda, d_out = g.d_out, d_in = g.d_in, y_dtype = g.parts > 1 ? kF32 : g.y_dtype;
-    void* Y = g.parts > 1 ? (void*)(g.partial + (int64_t)part * g.M * (GRAD ? g.d_in : g.d_out)) : g.Y;
+    void* Y = g.parts > 1 ? (void*)(g.partial + (int64_t)part * g.M * g.pitch) : g.Y;
     const int N = GRAD ? d_in : d_out;
     const int n0 = tile_n * kTileN;
     // the steps of this part of the contraction: an even number of them, at least 2
@@ -402,7 +428,11 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
                 for (int h = 0; h < FN; ++h) acc[f][h][r] *= x;
             }
     }
-    store_wave_tile<FM>(acc, (uint16_t*)tile_smem + wave * 32 * kGemmLDK, Y, y_dtype, m0, n0 + wn * 64, t.end, N, lane);
+    const int o0 = n0 + wn * 64;
+    if (store_tile_16bit<FM>(acc, (uint16_t*)tile_smem + wave * 32 * kGemmLDK, Y, y_dtype, m0, o0, t.end, N, lane)) return;
+    if (y_dtype == kF32) store_rows<kF32, FM>(acc, Y, g.parts > 1 ? g.pitch : N, m0, o0, t.end, N, lane);
+    else if (y_dtype == kBF16) store_rows<kBF16, FM>(acc, Y, N, m0, o0, t.end, N, lane);
+    else store_rows<kF16, FM>(acc, Y, N, m0, o0, t.end, N, lane);
 }
 
 // A tile of fewer tokens takes as many MFMA tiles as they need: the ends of ragged experts cost what they are.
@@ -414,7 +444,7 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
                    int n_tiles, int parts, int sign_ld)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
-    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts, sign_ld};
+    const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts, sign_ld, n_tiles * kTileN};
     ExpertTile t;
     int tile_n;
     {
@@ -436,40 +466,36 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
 template <int YDT>
 __global__ void __launch_bounds__(256)
 experts_sum_kernel(const float* __restrict__ partial, const float* __restrict__ inverse, const int* __restrict__ offsets, void* __restrict__ Y,
-                   int M, int E, int N, int parts, int blocks)
+                   int M, int E, int N, int pitch, int parts, int blocks)
 {
     const int m = blockIdx.x / blocks, n = (blockIdx.x % blocks * 256 + threadIdx.x) * 4;
     if (n >= N || (offsets != nullptr && (m < offsets[0] || m >= offsets[E]))) return;
     const float x = inverse != nullptr ? inverse[m] : 1.f;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    const int64_t at = (int64_t)m * N + n;
-    if ((N & 3) == 0) {
-        for (int p = 0; p < parts; ++p) {
-            const float4v a = *(const float4v*)(partial + (int64_t)p * M * N + at);
+    for (int p = 0; p < parts; ++p) {
+        const float4v a = *(const float4v*)(partial + ((int64_t)p * M + m) * pitch + n);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += a[e];
-        }
-    } else {
-        for (int p = 0; p < parts; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < N) sum[e] += partial[(int64_t)p * M * N + at + e];
+        for (int e = 0; e < 4; ++e) sum[e] += a[e];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (n + e < N) store_y<YDT>(Y, at + e, sum[e] * x);
+        if (n + e < N) store_y<YDT>(Y, (int64_t)m * N + n + e, sum[e] * x);
 }
 
-// Parts of the contraction: tiles that leave most of the 256 CUs idle are cut into as many parts as fill them, of four steps at
-// least (one expert, 64 tokens, 4096 x 4096 fp16, 16 tiles: 52 us, in 16 parts 26; 8 experts, 128 tiles: 75, in two parts 68).  More
-// parts than that cost more than they give (12 fine-tunes, 1501 tokens, 192 tiles of unequal length: 118, in three parts 142; 16
-// experts of 64 tokens, 256 tiles: 119, in two parts 161).  The sums take at most 64 MiB of workspace.
+int64_t experts_pitch(int64_t N) { return (N + kTileN - 1) / kTileN * kTileN; }
+
+// Parts of the contraction: tiles that leave most of the 256 CUs idle are cut into as many parts as fill three quarters of them, or
+// all where experts have few tokens and their sums are short, of six (four) steps at least.  us in 1, 2, 3, 4, 6, 8 and 12 parts: 2 experts,
+// 456 tokens, 1667 x 3328 fp16, 14 tiles: 79, 48, 38, 34, 30, 30, 38; 64 tokens, input gradient of 11008 x 4096, 16 tiles: 142, 79, 57,
+// 46, 37, 32, 32; 1000 tokens, 4096 x 4096, 64 tiles: 93, 64, 58, 61, 76, 86, 104; 17 experts, 2741 tokens, input gradient of 982 x 1280, 85
+// tiles: 43, 42, 51, 55.  The sums take at most 64 MiB of workspace.
 int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K)
 {
     if (M == 0) return 1;
     const int64_t met = std::min(E, M), tiles = (N + kTileN - 1) / kTileN * met * ((M + met * kTileM - 1) / (met * kTileM));
     const int64_t steps = experts_padded(K) / kTileK;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({16, 256 / tiles, steps / 4}));
+    const bool few = M <= 128 * met;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({12, (few ? 256 : 192) / tiles, steps / (few ? 4 : 6)}));
 }
 
 template <int WDT, int AXIS, bool GRAD>
@@ -509,7 +535,7 @@ int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int l
     const int64_t N = grad ? c.d_in : c.d_out, blocks = (N + 1023) / 1024;
 #define PDELTA_GO(YDT)                                                                                                              \
     hipLaunchKernelGGL(experts_sum_kernel<YDT>, dim3((unsigned)(c.M * blocks)), dim3(256), 0, stream, partial, inverse, c.offsets, c.out, \
-                       (int)c.M, (int)c.E, (int)N, parts, (int)blocks)
+                       (int)c.M, (int)c.E, (int)N, (int)experts_pitch(N), parts, (int)blocks)
     if (c.out_dtype == kF32) PDELTA_GO(kF32);
     else if (c.out_dtype == kBF16) PDELTA_GO(kBF16);
     else PDELTA_GO(kF16);

@@ -77,11 +77,13 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
         uint32_t pcol[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) pcol[q] = (uint32_t)min(p0 + piece[q], (dP - 1) / 8 * 8) * 2u;
+        if (wave * 8 <= (most | 15)) {                // (a wave whose tokens are behind the last ones' 16 has nothing to bring)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t row = (uint32_t)min(tok + q * 2, most);
-            load_lds_16(lds0 + stage + (wave * 4 + q) * 1024, row * (uint32_t)p_ld * 2u + pcol[q & 1], pb);
-            load_lds_16(lds0 + stage + kGradOperand + (wave * 4 + q) * 1024, row * (uint32_t)q_ld * 2u + qcol[q & 1], qb);
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t row = (uint32_t)min(tok + q * 2, most);
+                load_lds_16(lds0 + stage + (wave * 4 + q) * 1024, row * (uint32_t)p_ld * 2u + pcol[q & 1], pb);
+                load_lds_16(lds0 + stage + kGradOperand + (wave * 4 + q) * 1024, row * (uint32_t)q_ld * 2u + qcol[q & 1], qb);
+            }
         }
         if (++asked_step == n_steps) {
             asked_step = 0;
@@ -93,6 +95,7 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
     auto clear_behind = [&](int tile, int s, uint32_t stage) {
         const int p0 = (first_tile + tile) * kGradTile;
         if ((s + 1) * kGradTokens <= n && p0 + kGradTile <= dP) return;       // uniform
+        if (wave * 8 > ((n - 1 - s * kGradTokens) | 15)) return;              // these tokens are not multiplied
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const bool none = s * kGradTokens + tok + q * 2 >= n;
@@ -199,18 +202,23 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[f][h][r] = 0.f;
         }
-        read_frags(cur, 1);
+        const int left = n - s * kGradTokens;         // 16 tokens for each quarter of a step: the last one may have fewer quarters
+        if (left > 16) read_frags(cur, 1);
         __builtin_amdgcn_sched_barrier(0);
         multiply(0);
         __builtin_amdgcn_sched_barrier(0);
-        read_frags(cur, 2);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1);
-        __builtin_amdgcn_sched_barrier(0);
-        read_frags(cur, 3);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(2);
-        __builtin_amdgcn_sched_barrier(0);
+        if (left > 16) {
+            if (left > 32) read_frags(cur, 2);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (left > 32) {
+            if (left > 48) read_frags(cur, 3);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         wait_loads<0>();
 #pragma unroll
         for (int h = 0; h < (AXIS == 0 ? FQ : 1); ++h)            // (a use of the signs where all loads have been waited for anyway)
@@ -223,7 +231,7 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
         if (AXIS == 1 && s == 0) *(uint4v*)(tile_signs + threadIdx.x * 4) = (uint4v){sw[0][0], sw[0][1], sw[0][2], sw[0][3]};
         if (now + 2 < all) request(cur);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(3);
+        if (left > 48) multiply(3);
         __builtin_amdgcn_sched_barrier(0);
         if (after == 0) {
             add_tile();

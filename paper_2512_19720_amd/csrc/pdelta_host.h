@@ -159,9 +159,10 @@ int experts_decode_tokens(int64_t M, int64_t E, int64_t d_in, int dtype);
 int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream);
 
 // The products on tiles of 256 outputs with direct loads: A holds fp16 rows of lda values, a multiple of 128; inverse: a factor for
-// each row of the outputs, or NULL; partial: parts x M x (outputs) fp32 where the contraction, K long, is cut into more than one
-// part; sign_ld: bytes between the signs of two output rows (c.B_packed), forward a multiple of 16.
+// each row of the outputs, or NULL; partial: parts x M x experts_pitch(outputs) fp32 where the contraction, K long, is cut into
+// more than one part; sign_ld: bytes between the signs of two output rows (c.B_packed), forward a multiple of 16.
 int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K);
+int64_t experts_pitch(int64_t N);
 int launch_experts_big(const ExpertsCall& c, bool grad, const uint16_t* A, int lda, const float* inverse, float* partial, int parts,
                        int sign_ld, hipStream_t stream);
 
