@@ -140,18 +140,22 @@ struct ExpertTiles {
         const int64_t cost = (M * FULL / BM + 1 + 3 * std::min(E, M)) * n_tiles;
         return (cost / 8 + 2) / 3 + 1;
     }
-    __device__ __forceinline__ void tile(int number, ExpertTile& out, int& tile_n)
+    // Tile `number`; false (all lanes) if the offsets, which nobody has checked, do not add up to one.
+    __device__ __forceinline__ bool tile(int number, ExpertTile& out, int& tile_n)
     {
         const int n = n_tiles;
         const int l = seek([&](int upto, int) { return upto * n > number; });
+        if (l < 0) return false;
         const int mine = __builtin_amdgcn_readlane(tiles, l);
         const int place = number - (tiles_before + __builtin_amdgcn_readlane(tiles_upto, l) - mine) * n;
+        if (mine <= 0 || place < 0 || place / n >= mine) return false;
         tile_n = place / mine;
         out.tiles = mine;
         out.index = place % mine;
         out.expert = e0 + l;
         out.row0 = __builtin_amdgcn_readlane(first, l) + out.index * BM;
         out.end = __builtin_amdgcn_readlane(end, l);
+        return true;
     }
 };
 

@@ -1,8 +1,12 @@
 // Products of tokens sorted by expert with W_hat (forward) or its transpose (GRAD) on tiles of up to 256 tokens x 256 outputs x 64
-// of the contraction, 8 waves, all global traffic as direct loads into LDS.  The arithmetic is that of
-// pdelta_experts_gemm.hip, and the schedule that of the dense 256 x 256 prefill kernel: two LDS stages; a wave turns the pieces of
-// W_b that it has itself loaded into W_hat in place, between its matrix instructions; one barrier per step, three quarters into
-// it, which publishes step s + 1 and frees the stage of step s for step s + 2.
+// of the contraction, 8 waves.  The arithmetic is that of pdelta_experts_gemm.hip.  Tokens, signs and scales come by direct loads into
+// LDS; W_b comes through registers and goes to LDS as W_hat, between the matrix instructions of the step before; one barrier per step,
+// three quarters into it, which publishes step s + 1 and frees the stages of step s.
+//
+// What bounds it: full tiles of one expert (2048 tokens, 8192 x 4096 fp16, one round of 256 tiles) run at 1040 TFLOP/s, 86 % of what a
+// large library product reaches on this card, the matrix cores busy 56 % of the time at clocks that power limits (1.7 GHz).  Uneven
+// experts lose more: 2048 tokens x 2 of 8 experts, 14336 x 4096 bf16, 700 TFLOP/s: 12 % of the tiles' rows are no tokens, the
+// busiest CUs work half a tile longer than the others, and bf16 weights cost 10 % for their conversion.  HBM is not it: 0.89 GB in 650 us.
 //
 // The tokens come as fp16 rows of a multiple of 128 values (prepared ones, or X and dY themselves); forward, the signs as rows of a
 // multiple of 16 bytes.
@@ -22,7 +26,6 @@
 #include "pdelta_lds_load.h"
 
 namespace pdelta {
-
 
 constexpr int kTileM = 256, kTileN = 256, kTileK = 64;
 constexpr int kWBytes = kTileN * kTileK * 2;          // W_b in a stage
@@ -450,8 +453,7 @@ experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restr
     {
         ExpertTiles<kTileM> list{offsets, E, M, n_tiles * parts};     // a part is a tile of its own here
         const int stop = list.range((int)blockIdx.x % kXcds), number = list.at + (int)blockIdx.x / kXcds;
-        if (number >= stop) return;                   // whole workgroup
-        list.tile(number, t, tile_n);
+        if (number >= stop || !list.tile(number, t, tile_n)) return;          // whole workgroup
     }
     const int part = tile_n % parts;
     tile_n /= parts;

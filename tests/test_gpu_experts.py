@@ -116,7 +116,7 @@ def test_what_is_not_a_number_stays_in_its_row(dtype):
 def test_offsets_out_of_order_stay_in_bounds():
     """No meaning, but no access outside the buffers: the guards around the outputs hold."""
     c = make([40, 30, 20], 96, 128, BF16, ROW, 10)
-    for offsets in ([0, 500, 20, 90], [-7, 10, 90, 90], [90, 40, 20, 0], [2 ** 31 - 1, -2 ** 31, 50, 2 ** 31 - 1]):
+    for offsets in ([0, 500, 20, 90], [0, 90, 0, 90], [-7, 10, 90, 90], [90, 40, 20, 0], [2 ** 31 - 1, -2 ** 31, 50, 2 ** 31 - 1]):
         c["offsets"] = torch.tensor(offsets, dtype=torch.int32, device=DEV)
         pad = torch.full((90 + 40, 96), 7.0, dtype=BF16, device=DEV)
         linear(c, ROW, BF16, out=pad[20:110])
@@ -216,3 +216,57 @@ def test_grad_v_in_runs(counts, d_out, d_in, dtype, axis):
     got = pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis)
     held(got, *grad_v64(c["X"], c["dY"], c["offsets"], c["B"], axis), f"grad_v {counts} {d_out}x{d_in} {dtype} axis {axis}")
     assert torch.equal(got, pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], axis))
+
+
+@pytest.mark.parametrize("dtype,d_in", [(F16, 96), (BF16, 384)])
+def test_many_experts(dtype, d_in):
+    """More experts than lanes of a wave, on the decode tiles and on the large ones."""
+    counts = [(7 * k) % 41 + 17 for k in range(150)]
+    c = make(counts, 72, d_in, dtype, ROW, 17, before=3, behind=5)
+    check_products(c, ROW, dtype, f"150 experts {dtype}")
+    c = make([k % 3 for k in range(300)], 40, 128, dtype, COL, 18)
+    check_products(c, COL, dtype, f"300 experts {dtype}")
+    got = pd.pdelta_grad_v_experts(c["X"], c["dY"], c["offsets"], c["B"], COL)
+    held(got, *grad_v64(c["X"], c["dY"], c["offsets"], c["B"], COL), "grad_v of 300 experts")
+
+
+def test_offsets_that_all_name_everything():
+    """Many experts that each claim all tokens: sums over them pass 31 bits; no meaning, no access outside the buffers."""
+    E, M, d = 2048, 4096, 64
+    X = torch.zeros(M, d, dtype=F16, device=DEV)
+    offsets = torch.tensor([0, M] * (E // 2) + [0], dtype=torch.int32, device=DEV)
+    W = torch.zeros(d, d, dtype=F16, device=DEV)
+    B, v = torch.zeros(E, d, d // 32, dtype=torch.int32, device=DEV), torch.zeros(E, d, dtype=F16, device=DEV)
+    pad = torch.full((M + 600, d), 7.0, dtype=F16, device=DEV)
+    pd.pdelta_linear_experts(X, offsets, W, B, v, ROW, out=pad[300:M + 300])
+    assert (pad[:300] == 7.0).all() and (pad[M + 300:] == 7.0).all()
+    pd.pdelta_grad_x_experts(X, offsets, W, B, v, ROW, out=pad[300:M + 300])
+    assert (pad[:300] == 7.0).all() and (pad[M + 300:] == 7.0).all()
+
+
+def test_experts_beyond_two_to_the_31_weights():
+    """The last expert's weights, signs and tokens like those of a call of their own."""
+    E, d_out, d_in = 40, 8192, 8192                   # 2.7e9 weights
+    g = torch.Generator(device=DEV).manual_seed(5)
+    W = torch.zeros(E, d_out, d_in, dtype=BF16, device=DEV)
+    B = torch.zeros(E, d_out, d_in // 32, dtype=torch.int32, device=DEV)
+    v = torch.full((E, d_out), 0.001, dtype=F16, device=DEV)
+    W[-1] = torch.randn(d_out, d_in, generator=g, device=DEV) * 0.02
+    B[-1] = torch.randint(-2 ** 31, 2 ** 31, (d_out, d_in // 32), generator=g, device=DEV).to(torch.int32)
+    X = torch.randn(70, d_in, generator=g, device=DEV).to(BF16)
+    dY = torch.randn(70, d_out, generator=g, device=DEV).to(BF16)
+    for n in (5, 70):                                 # decode tiles and large ones
+        offsets = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+        offsets[-1] = n
+        one = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        last = (W[-1:].contiguous(), B[-1:].contiguous(), v[-1:].contiguous())
+        for grad, t in ((False, X), (True, dY)):
+            f = pd.pdelta_grad_x_experts if grad else pd.pdelta_linear_experts
+            got, want = f(t[:n], offsets, W, B, v, ROW, out_dtype=F32), f(t[:n], one, *last, ROW, out_dtype=F32)
+            # (a call of 40 experts may take other tiles than one of one: each within its bound of the exact value, 2^-11 of the sum of sizes)
+            bound = t[:n].abs().float() @ (last[0][0].abs().float() + 0.001).T if not grad else t[:n].abs().float() @ (last[0][0].abs().float() + 0.001)
+            assert ((got - want).abs() <= bound * 2.0 ** -10).all()
+        gv = pd.pdelta_grad_v_experts(X[:n], dY[:n], offsets, B, ROW)
+        assert torch.equal(gv[:-1], torch.zeros_like(gv[:-1]))
+        want = pd.pdelta_grad_v_experts(X[:n], dY[:n], one, last[1], ROW)
+        assert ((gv[-1] - want[0]).abs() <= want.abs().max() * 1e-4).all()

@@ -63,3 +63,12 @@ def test_spilled_registers_of_every_kernel(tmp_path):
         assert scratch <= (4 * SPILLS[family] + 16 if family in SPILLS else 0), (name, scratch)
     assert {"grad_big_kernel", "grad_tile_pipe_kernel", "linear_skinny_kernel", "linear_skinny_staged_kernel",
             "linear_gemm_small_kernel", "pack_main_kernel", "patch_kernel"} | set(SPILLS) <= seen
+
+
+def test_kernels_of_sorted_tokens_do_not_spill(tmp_path):
+    """Their waits count loads that were asked for since: a reload from scratch memory would be one of them."""
+    found = {n: e for n, e in kernels(tmp_path).items() if "experts_big_kernel" in n or "experts_grad_kernel" in n or "experts_skinny_kernel" in n}
+    assert sum("experts_big_kernel" in n for n in found) == 8                # two operand types, two kinds of scales, two directions
+    assert sum("experts_grad_kernel" in n for n in found) == 4 and sum("experts_skinny_kernel" in n for n in found) == 12
+    for name, entry in found.items():
+        assert re.search(r"\.vgpr_spill_count:\s+0\b", entry) and re.search(r"\.private_segment_fixed_size:\s+0\b", entry), name
