@@ -285,7 +285,6 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
     using I1 = std::integral_constant<int, 1>;
     using I2 = std::integral_constant<int, 2>;
     using I3 = std::integral_constant<int, 3>;
-    constexpr int VALU = ((WDT == kBF16 ? 13 : 7) * 8 + FM * FN - 1) / (FM * FN);     // vector instructions after each MFMA of a quarter
     const int last = n_steps - 1;
 
     // The fences keep the LDS reads above the MFMAs, the conversion between them, and the loads in their order: a wait counts the
@@ -329,7 +328,6 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             __builtin_amdgcn_sched_barrier(0);
             multiply(1);
             convert_w(w_stage(P + 1), Next{});
-            interleave<FM * FN, VALU>();
             __builtin_amdgcn_sched_barrier(0);
             read_frags(a_stage(P), w_stage(P), I3{});
             __builtin_amdgcn_sched_barrier(0);
@@ -390,7 +388,7 @@ __device__ __forceinline__ void experts_tile(const TileArgs& g, const ExpertTile
             read_frags(a_stage(P), w_stage(P), I2{});
             __builtin_amdgcn_sched_barrier(0);
             multiply(1);
-            if constexpr (MORE) { convert_w(w_stage(P + 1), Next{}); interleave<FM * FN, VALU>(); }
+            if constexpr (MORE) convert_w(w_stage(P + 1), Next{});        // (the compiler's own order among the MFMAs: 1-2 % better than a fixed one)
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (REQ && AHEAD == 1) request_w(s + 2, I0{});
             read_frags(a_stage(P), w_stage(P), I3{});
