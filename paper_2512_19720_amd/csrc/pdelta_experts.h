@@ -55,19 +55,20 @@ __device__ __forceinline__ bool find_expert_tile(const int* __restrict__ offsets
     return false;
 }
 
-// The tiles of a product, up to BM tokens x one output tile each, numbered expert by expert, then by output tile, then by token
+// The tiles of a product, up to `height` tokens x one output tile each, numbered expert by expert, then by output tile, then by token
 // tile (an expert's last token tile may be a short one), dealt to the 8 XCDs in contiguous ranges of about the same cost: the CUs
 // of an XCD then share panels of weights in its L2.  A tile of 64 f tokens costs f + 2, as measured next to a full one.
-template <int BM>
 struct ExpertTiles {
-    static constexpr int FULL = BM / 64 + 2;
     const int* offsets;
     int E, M, n_tiles;
+    int height;                                       // 256, 192 or 128
     int at, e0;                                       // this range's next tile; first expert of the chunk that the lanes hold
     int first, end, tiles, cost;                      // of expert e0 + lane
     int tiles_upto, cost_upto;                        // sums up to and with it
     int tiles_before, cost_before;                    // sums of the chunks before
 
+    __host__ __device__ static int full_cost(int rows) { return (rows + 63) / 64 + 2; }
+    __device__ __forceinline__ int full() const { return full_cost(height); }
     __device__ __forceinline__ int lane() const { return threadIdx.x & 63; }
     __device__ __forceinline__ static int prefix(int x)
     {
@@ -78,18 +79,26 @@ struct ExpertTiles {
         }
         return x;
     }
-    __device__ __forceinline__ void chunk(int from, int tiles_sum, int cost_sum)
+    __device__ __forceinline__ void rows_of(int from)
     {
         e0 = from;
-        tiles_before = tiles_sum;
-        cost_before = cost_sum;
         expert_rows(offsets, min(e0 + lane(), E - 1), M, first, end);
         if (e0 + lane() >= E) end = first;
-        const int rest = (end - first) % BM;
-        tiles = (end - first) / BM + (rest > 0);
-        cost = (end - first) / BM * FULL + (rest > 0 ? (rest + 63) / 64 + 2 : 0);
+    }
+    __device__ __forceinline__ void count()
+    {
+        const int whole = (int)((uint32_t)(end - first) / (uint32_t)height), rest = end - first - whole * height;
+        tiles = whole + (rest > 0);
+        cost = whole * full_cost(height) + (rest > 0 ? full_cost(rest) : 0);
         tiles_upto = prefix(tiles);
         cost_upto = prefix(cost);
+    }
+    __device__ __forceinline__ void chunk(int from, int tiles_sum, int cost_sum)
+    {
+        tiles_before = tiles_sum;
+        cost_before = cost_sum;
+        rows_of(from);
+        count();
     }
     __device__ __forceinline__ int chunk_tiles() const { return __builtin_amdgcn_readlane(tiles_upto, kWave - 1); }
     __device__ __forceinline__ int chunk_cost() const { return __builtin_amdgcn_readlane(cost_upto, kWave - 1); }
@@ -113,8 +122,44 @@ struct ExpertTiles {
         if (l < 0) return all;
         const int mine = __builtin_amdgcn_readlane(tiles, l), each = __builtin_amdgcn_readlane(cost, l);
         const int rest = bound - (cost_before + __builtin_amdgcn_readlane(cost_upto, l) - each) * n;
-        const int behind = (rest % each + FULL - 1) / FULL;       // token tiles that start before the bound
+        const int behind = (rest % each + full() - 1) / full();       // token tiles that start before the bound
         return (tiles_before + __builtin_amdgcn_readlane(tiles_upto, l) - mine) * n + rest / each * mine + min(behind, mine);
+    }
+    // Twice the time in which the 256 CUs work `tiles` off, the largest of cost `largest`, `cost` all together: whole rounds if they
+    // are alike or there is one round, else a CU's mean and half a tile.
+    __host__ __device__ static int64_t finish(int64_t tiles, int64_t cost, int largest, bool alike)
+    {
+        return alike || tiles <= 256 ? 2 * ((tiles + 255) / 256) * largest : cost / 128 + largest;
+    }
+    // A smaller height reads the weights more often: it is taken for a gain of an eighth.
+    __host__ __device__ static bool gains(int64_t t, int64_t least) { return t * 8 <= least * 7; }
+    // Heights by the tokens that the experts have, of one wave's lanes of experts.  See launch_big_tiles.
+    __device__ __forceinline__ void choose_height()
+    {
+        rows_of(0);
+        int most = 0;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) most += __ballot(end - first > 64 * f) != 0;
+        int best = height;
+        int64_t least = 0;
+        if (most > 2)
+            for (int h = 256; h >= 128; h -= 64) {
+                height = h;
+                count();
+                const int64_t t = finish((int64_t)chunk_tiles() * n_tiles, (int64_t)chunk_cost() * n_tiles, min(most, h / 64) + 2, false);
+                if (h == 256 || gains(t, least)) { best = h; least = t; }
+            }
+        height = best;
+    }
+    static int height_of_one(int64_t M, int64_t n_tiles)
+    {
+        int best = 256;
+        int64_t least = 0;
+        for (int h = 256; h >= 128 && (M + 255) / 256 * n_tiles <= 768; h -= 64) {                // (three rounds)
+            const int64_t t = finish((M + h - 1) / h * n_tiles, 0, full_cost((int)std::min<int64_t>(M, h)), true);
+            if (h == 256 || gains(t, least)) { best = h; least = t; }
+        }
+        return best;
     }
     // Range [at, stop) of XCD `xcd`.
     __device__ __forceinline__ int range(int xcd)
@@ -133,11 +178,13 @@ struct ExpertTiles {
         at = first_at(bound(xcd), all);
         return stop;
     }
-    // The most tiles that a range can have: M tokens cost FULL for each BM of them and, the last tile of each expert, at most 3 more;
+    // The most tiles that a range can have: M tokens cost full() for each `height` of them and, the last tile of each expert, at most 3 more;
     // the cheapest tile costs 3.
-    static int64_t most_in_a_range(int64_t M, int64_t E, int64_t n_tiles)
+    static int64_t most_in_a_range(int64_t M, int64_t E, int64_t n_tiles, int height)
     {
-        const int64_t cost = (M * FULL / BM + 1 + 3 * std::min(E, M)) * n_tiles;
+        // one expert: runs of its token tiles, one for each output tile, in eight parts that may begin and end inside a run
+        if (E == 1) return ((n_tiles + 7) / 8 + 1) * ((M + height - 1) / height);
+        const int64_t cost = (M * full_cost(height) / height + 1 + 3 * std::min(E, M)) * n_tiles;
         return (cost / 8 + 2) / 3 + 1;
     }
     // Tile `number`; false (all lanes) if the offsets, which nobody has checked, do not add up to one.
@@ -153,7 +200,7 @@ struct ExpertTiles {
         out.tiles = mine;
         out.index = place % mine;
         out.expert = e0 + l;
-        out.row0 = __builtin_amdgcn_readlane(first, l) + out.index * BM;
+        out.row0 = __builtin_amdgcn_readlane(first, l) + out.index * height;
         out.end = __builtin_amdgcn_readlane(end, l);
         return true;
     }

@@ -442,20 +442,21 @@ __global__ void __launch_bounds__(512, 2)
 experts_big_kernel(const uint16_t* __restrict__ A, int lda, const float* __restrict__ inverse, const int* __restrict__ offsets,
                    const uint16_t* __restrict__ W_b, int64_t w_stride, const uint32_t* __restrict__ B_packed,
                    const uint16_t* __restrict__ v, void* __restrict__ Y, float* __restrict__ partial, int M, int E, int d_out, int d_in, int y_dtype,
-                   int n_tiles, int parts, int sign_ld)
+                   int n_tiles, int parts, int sign_ld, int height)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char tile_smem[];
     const TileArgs g{A, lda, inverse, W_b, w_stride, B_packed, v, Y, partial, M, d_out, d_in, y_dtype, parts, sign_ld, n_tiles * kTileN};
     ExpertTile t;
-    int tile_n;
+    int tile_n, rows;
     {
-        ExpertTiles<kTileM> list{offsets, E, M, n_tiles * parts};     // a part is a tile of its own here
+        ExpertTiles list{offsets, E, M, n_tiles * parts, height > 0 ? height : kTileM};     // a part is a tile of its own here
+        if (height == 0) list.choose_height();
         const int stop = list.range((int)blockIdx.x % kXcds), number = list.at + (int)blockIdx.x / kXcds;
         if (number >= stop || !list.tile(number, t, tile_n)) return;          // whole workgroup
+        rows = min(t.end - t.row0, list.height);
     }
     const int part = tile_n % parts;
     tile_n /= parts;
-    const int rows = t.end - t.row0;
     if (rows > 192) experts_tile<WDT, AXIS, GRAD, 4>(g, t, tile_n, part, tile_smem);
     else if (rows > 128) experts_tile<WDT, AXIS, GRAD, 3>(g, t, tile_n, part, tile_smem);
     else if (rows > 64) experts_tile<WDT, AXIS, GRAD, 2>(g, t, tile_n, part, tile_smem);
@@ -498,19 +499,26 @@ int experts_parts(int64_t M, int64_t E, int64_t N, int64_t K)
     return (int)std::max<int64_t>(1, std::min<int64_t>({12, (few ? 256 : 192) / tiles, steps / (few ? 4 : 6)}));
 }
 
+// Tokens of a full tile: 256, or as many of 192 and 128 as let the CUs finish an eighth sooner by the tiles' costs.  For one expert the
+// host takes its M tokens for it; for up to 64, of which about one round of tiles is expected, the kernel (0) looks at the offsets.
+// us with 256 and with the rule: input gradient of 4096 x 11008, 777 tokens 118, 105 (192); 2048 tokens 238, 225 (192); 4 experts, 1500
+// tokens, 4096 x 4096 bf16 110, 94 (128); 12 experts, 1501 tokens 114, 106 (192).  More rounds of uneven experts gain nothing and
+// pay for the look: 16 experts, 3000 tokens 116, 123; 8 experts, 1024 tokens, 14336 x 4096 288, 295.
 template <int WDT, int AXIS, bool GRAD>
 static int launch_big_tiles(const ExpertsCall& c, const uint16_t* A, int lda, const float* inverse, float* partial, int parts, int sign_ld,
                             hipStream_t stream)
 {
     constexpr int lds = kTileLds;
     const int64_t n_tiles = ((GRAD ? c.d_in : c.d_out) + kTileN - 1) / kTileN;
-    const int64_t most = ExpertTiles<kTileM>::most_in_a_range(c.M, c.E, n_tiles * parts), blocks = most * kXcds;
+    const bool few = (c.M / kTileM + std::min(c.E, c.M) / 2) * n_tiles <= 256;
+    const int height = parts > 1 || c.M <= 128 ? kTileM : c.E == 1 ? ExpertTiles::height_of_one(c.M, n_tiles) : c.E <= kWave && few ? 0 : kTileM;
+    const int64_t most = ExpertTiles::most_in_a_range(c.M, c.E, n_tiles * parts, height > 0 ? height : 128), blocks = most * kXcds;
     if (most > (1 << 24)) return -2;                  // (costs are summed in 32 bits)
     auto kernel = experts_big_kernel<WDT, AXIS, GRAD>;
     static unsigned lds_opted_in = 0;                 // per template instance: one kernel
     if (opt_in_dynamic_lds((const void*)kernel, lds, &lds_opted_in) != 0) return -1;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(512), lds, stream, A, lda, inverse, c.offsets, (const uint16_t*)c.W_b, c.w_stride,
-                       c.B_packed, c.v, c.out, partial, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles, parts, sign_ld);
+                       c.B_packed, c.v, c.out, partial, (int)c.M, (int)c.E, (int)c.d_out, (int)c.d_in, c.out_dtype, (int)n_tiles, parts, sign_ld, height);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

@@ -270,3 +270,30 @@ def test_experts_beyond_two_to_the_31_weights():
         assert torch.equal(gv[:-1], torch.zeros_like(gv[:-1]))
         want = pd.pdelta_grad_v_experts(X[:n], dY[:n], one, last[1], ROW)
         assert ((gv[-1] - want[0]).abs() <= want.abs().max() * 1e-4).all()
+
+
+# tokens around the ends of tiles of 128, 192 and 256; one expert (chosen before the launch) and several (chosen in it); the last three: 192, of one expert in one round
+# of tiles on 256 CUs, in two, and of several
+@pytest.mark.parametrize("counts,d_out,d_in", [([129], 300, 288), ([192], 520, 256), ([193], 96, 352), ([777], 512, 128), ([385, 0, 191], 260, 512),
+                                               ([129, 257, 1], 1024, 288), ([255, 128, 640, 0, 193], 320, 256), ([513, 96], 2050, 96),
+                                               ([900], 11008, 160), ([1500], 14336, 160), ([700, 300], 8300, 160)])
+def test_tiles_of_every_height(counts, d_out, d_in):
+    for k, (dtype, axis) in enumerate([(F16, ROW), (F16, COL), (BF16, ROW), (BF16, COL)]):
+        c = make(counts, d_out, d_in, dtype, axis, 900 + k + d_out, before=1, behind=2)
+        check_products(c, axis, dtype, f"{counts} {d_out}x{d_in} {dtype} axis {axis}")
+    d_out = (d_out + 31) // 32 * 32                     # (inputs come in words of 32)
+    c = make(counts, d_in, d_out, F16, ROW, 950 + d_out, before=3)
+    check_products(c, ROW, F16, f"{counts} {d_in}x{d_out}")
+
+
+def test_few_offsets_that_name_the_same_tokens():
+    M, d = 700, 128
+    X = torch.zeros(M, d, dtype=F16, device=DEV)
+    W = torch.zeros(d, d, dtype=F16, device=DEV)
+    B, v = torch.zeros(5, d, d // 32, dtype=torch.int32, device=DEV), torch.zeros(5, d, dtype=F16, device=DEV)
+    for offsets in ([0, M, 0, M, 0, M], [M, 0, 300, 100, 2 ** 31 - 1, -5]):
+        pad = torch.full((M + 600, d), 7.0, dtype=F16, device=DEV)
+        o = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+        pd.pdelta_linear_experts(X, o, W, B, v, ROW, out=pad[300:M + 300])
+        pd.pdelta_grad_x_experts(X, o, W, B, v, ROW, out=pad[300:M + 300])
+        assert (pad[:300] == 7.0).all() and (pad[M + 300:] == 7.0).all()
