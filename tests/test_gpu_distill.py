@@ -157,3 +157,17 @@ def test_rows_behind_two_to_the_31():
     loss_bound, grad_bound = distill_bounds(rest, ids_rest, top_rest, None, 1.0, 1.0)
     held(loss[-3:], want_loss.cpu().double(), 2 * loss_bound, "loss")
     held(grad[-3:], want_grad.cpu().double(), 2 * grad_bound, "grad")
+
+
+# rows that end at and behind what a workgroup keeps in registers, of more tokens than are split among workgroups
+@pytest.mark.parametrize("T,V,dtype", [(130, 16384, F16), (5, 16385, BF16), (40, 16399, F16), (129, 32769, BF16), (131, 65536, F16), (129, 65601, F16),
+                                       (130, 70001, BF16), (129, 81927, F16), (129, 81928, BF16), (129, 131099, F16), (129, 8192, F32), (3, 8196, F32),
+                                       (129, 40963, F32), (130, 40964, F32)])
+def test_rows_longer_than_what_is_kept(T, V, dtype):
+    logits, ids, top, g = make(T, V, 12, dtype, T + V)
+    logits[1::3, V // 2:] = float("-inf")
+    logits[2::5, :V - 3] = -60000.0                   # the largest of the row in its last words
+    top[logits.gather(1, ids.long()).isinf()] = float("-inf")
+    weight = torch.rand(T, generator=g).to(DEV)
+    weight[::7] = 0
+    check(logits, ids, top, weight, 1.3, 2.0, f"{T}x{V} {dtype}")
