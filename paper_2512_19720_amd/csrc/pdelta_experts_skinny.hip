@@ -1,6 +1,7 @@
 // Forward product of tokens sorted by expert where an expert has few of them (decode of a mixture of experts): the decode tile of
 // the dense layer, 16 MT tokens of one expert x 16 NT output rows, for every expert that has tokens.  Memory-bound: the weights
-// of every expert that is met are read once for each 16 MT tokens of its, and those of the others not at all.
+// of every expert that is met are read once for each 16 MT tokens of its, and those of the others not at all (32 tokens x 2 of 64 experts,
+// 2048 x 4096 bf16: 0.50 GB in 81 us, 6.2 TB/s).
 //
 // A workgroup first looks its expert up, a load and a prefix sum away from its first weight, and ends with a sum over its waves;
 // two stages of a wave (or two row tiles and one) leave room for two workgroups on a CU, which cover each other's ends.
