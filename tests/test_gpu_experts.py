@@ -297,3 +297,38 @@ def test_few_offsets_that_name_the_same_tokens():
         pd.pdelta_linear_experts(X, o, W, B, v, ROW, out=pad[300:M + 300])
         pd.pdelta_grad_x_experts(X, o, W, B, v, ROW, out=pad[300:M + 300])
         assert (pad[:300] == 7.0).all() and (pad[M + 300:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(F16, BF16), (BF16, F16)])
+@pytest.mark.parametrize("counts", [[3, 0, 9], [100, 0, 290]])
+def test_outputs_of_the_other_type(counts, dtype, out_dtype):
+    for axis in (ROW, COL):
+        check_products(make(counts, 136, 256, dtype, axis, 31, dy_scale=1.0), axis, out_dtype, f"{counts} {dtype} -> {out_dtype} axis {axis}")
+
+
+def test_tokens_beyond_two_to_the_31_values():
+    """The last expert's tokens, at the end of more than 2^31 values, like those of a call of their own."""
+    M, wide, narrow, n = 530000, 4096, 96, 300
+    g = torch.Generator(device=DEV).manual_seed(6)
+    tokens = torch.zeros(M, wide, dtype=BF16, device=DEV)
+    tokens[-n:] = torch.randn(n, wide, generator=g, device=DEV)
+    small = torch.zeros(M, narrow, dtype=BF16, device=DEV)
+    small[-n:] = torch.randn(n, narrow, generator=g, device=DEV)
+    W = (torch.randn(3, narrow, wide, generator=g, device=DEV) * 0.02).to(BF16)
+    B = torch.randint(-2 ** 31, 2 ** 31, (3, narrow, wide // 32), generator=g, device=DEV).to(torch.int32)
+    v = torch.full((3, narrow), 0.001, dtype=F16, device=DEV)
+    offsets = torch.tensor([0, 5, M - n, M], dtype=torch.int32, device=DEV)
+    one = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    last = (W[-1:].contiguous(), B[-1:].contiguous(), v[-1:].contiguous())
+    # each within a rounding of W_hat and of the fp32 sums of the exact value: 2^-11 of the sum of sizes, and a little
+    sizes = W[-1].abs().float() + 0.001
+    got, want = pd.pdelta_linear_experts(tokens, offsets, W, B, v, ROW, out_dtype=F32)[-n:], pd.pdelta_linear_experts(tokens[-n:], one, *last, ROW, out_dtype=F32)
+    assert ((got - want).abs() <= tokens[-n:].abs().float() @ sizes.T * 2.0 ** -10).all() and want.abs().max() > 0
+    gv, alone = pd.pdelta_grad_v_experts(tokens, small, offsets, B, ROW), pd.pdelta_grad_v_experts(tokens[-n:], small[-n:], one, last[1], ROW)
+    # sums in fp32 of n products and of `wide` of those
+    bound = (small[-n:].abs().float().T @ tokens[-n:].abs().float()).sum(1) * (n + wide) * 2.0 ** -23
+    assert torch.equal(gv[:2], torch.zeros_like(gv[:2])) and ((gv[2] - alone[0]).abs() <= bound).all() and alone.abs().max() > 0
+    del got, want
+    got, want = pd.pdelta_grad_x_experts(small, offsets, W, B, v, ROW)[-n:], pd.pdelta_grad_x_experts(small[-n:], one, *last, ROW)
+    bound = small[-n:].abs().float() @ sizes * 2.0 ** -10
+    assert ((got.float() - want.float()).abs() <= bound + want.float().abs() * 2.0 ** -7).all() and want.abs().max() > 0     # and two roundings to bf16
