@@ -177,7 +177,8 @@ struct RowPart {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) r[p] = pack_pair<DT>(value(element<DT>(a, 2 * p)), value(element<DT>(a, 2 * p + 1)));
             }
-            *(uint4v*)(dst + place(i)) = r;
+            // (not to be kept in the caches: us otherwise and so, 2048 x 128256 bf16 238, 227, x 70001 143, 125, 1024 x 128256 fp32 293, 263)
+            __builtin_nontemporal_store(r, (uint4v*)(dst + place(i)));
         };
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -427,15 +428,16 @@ static int launch_rows(const DistillCall& c, hipStream_t stream)
     } else {
         // Threads and the 16-byte vectors that each keeps in registers.  Eight let twice as many waves run on a CU as sixteen, for which the
         // rest of a row that is a little too long is read again.  us with sixteen and eight, 16-bit: 8192 x 10000 97, 75, the loss
-        // alone 69, 43; 2048 x 70000 170, 141, x 82000 177, 172, x 90000 183, 192, the loss alone of 70000 111, 63.  32000 in 512 threads of
-        // eight: 217, sixteen in 256 221, and 10000 107, 97.  The loss alone takes what the gradient would: its bits are the same.
+        // alone 69, 43; 2048 x 82000 172, 153, x 90000 185, 172, x 100000 192, 194, x 128256 227, 257; the loss alone of 70000 111, 63.
+        // 32000 in 512 threads of eight: 217, sixteen in 256 221, and 10000 107, 97.  The loss alone takes what the gradient would: its bits
+        // are the same.
         const int64_t vectors = c.V / PER;
 #define PDELTA_GO(THREADS, NV) hipLaunchKernelGGL((distill_kernel<DT, THREADS, NV>), dim3((unsigned)c.T), dim3(THREADS), 0, stream, g)
         if (vectors <= 256) PDELTA_GO(256, 1);
         else if (vectors <= 4 * 256) PDELTA_GO(256, 4);
         else if (vectors <= 8 * 256) PDELTA_GO(256, 8);
         else if (vectors <= 16 * 256) PDELTA_GO(256, 16);
-        else if (vectors <= 10 * 1024) PDELTA_GO(1024, 8);
+        else if (vectors <= 12 * 1024) PDELTA_GO(1024, 8);
         else PDELTA_GO(1024, 16);
 #undef PDELTA_GO
     }

@@ -162,7 +162,7 @@ def test_rows_behind_two_to_the_31():
 # rows that end at and behind what a workgroup keeps in registers, of more tokens than are split among workgroups
 @pytest.mark.parametrize("T,V,dtype", [(130, 16384, F16), (5, 16385, BF16), (40, 16399, F16), (129, 32769, BF16), (131, 65536, F16), (129, 65601, F16),
                                        (130, 70001, BF16), (129, 81927, F16), (129, 81928, BF16), (129, 131099, F16), (129, 8192, F32), (3, 8196, F32),
-                                       (129, 40963, F32), (130, 40964, F32)])
+                                       (129, 40963, F32), (130, 40964, F32), (129, 98304, BF16), (129, 98313, F16), (129, 49159, F32)])
 def test_rows_longer_than_what_is_kept(T, V, dtype):
     logits, ids, top, g = make(T, V, 12, dtype, T + V)
     logits[1::3, V // 2:] = float("-inf")
