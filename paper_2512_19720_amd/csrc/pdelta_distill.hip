@@ -2,16 +2,16 @@
 // q = softmax(z) over the vocabulary and p = softmax(top / tau) over the teacher's words that are in use:
 //   loss    = tau^2 w sum_j p_j (log p_j - log q[id_j])
 //   grad[i] = scale tau w (q[i] - sum_{j: id_j = i} p_j)
-// All of it is in fp32; sums over the vocabulary are taken relative to a largest logit.
+// All of it is in fp32; sums over the vocabulary are taken relative to a large logit.
 //
-// Bound by memory: logits once in, gradient once out (2048 x 128256 bf16, three tenths of the tokens without weight, 203 us: 0.38 GB read
-// and 0.53 written, 4.5 TB/s; a copy of 1 GiB reaches 5.2.  The loss alone of 640 x 32000 fp16 in 13.6 us: the launch, and 2.5 rows for
+// Bound by memory: logits once in, gradient once out (2048 x 128256 bf16, three tenths of the tokens without weight, 193 us: 0.38 GB read
+// and 0.53 written, 4.7 TB/s; a copy of 1 GiB reaches 5.2.  The loss alone of 640 x 32000 fp16 in 13 us: the launch, and 2.5 rows for
 // each CU).  A workgroup keeps its part of the row in registers, as the 16-byte vectors it was loaded as, between the sum over the
-// vocabulary and the gradient; what does not fit is read again.  Every wave sums relative to its own largest logit, and the
+// vocabulary and the gradient; what does not fit is read again.  Every wave sums relative to a large logit of its own, and the
 // waves meet once; the first wave deals with the teacher's words meanwhile.  The gradient is written as if the teacher had named no
 // word, and the words' own entries again after a barrier.
 //
-// Of few tokens, a long row is split among workgroups: one launch leaves every part's largest logit and sum (and the
+// Of few tokens, a long row is split among workgroups: one launch leaves a large logit and the sum of every part (and the
 // words' logits, since the gradient may replace the logits) in the workspace, a second one joins them in their order.
 #include <algorithm>
 #include <cmath>
@@ -87,7 +87,7 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-// Largest logit and sum of exponentials relative to it; (-inf, 0) is nothing.
+// A large logit and the sum of exponentials relative to it; (-inf, 0) is nothing.
 struct Sum { float most, total; };
 __device__ __forceinline__ Sum join(Sum a, Sum b, Temperature t)
 {
@@ -136,31 +136,42 @@ struct RowPart {
     __device__ __forceinline__ int64_t place(int64_t i) const { return (first + (i * THREADS + threadIdx.x) * PER) * (DT == kF32 ? 4 : 2); }
     __device__ __forceinline__ uint4v vector(int64_t i) const { return *(const uint4v*)(src + place(i)); }
 
-    // The wave's largest logit, and the sum relative to it (every lane has both).
+    // A large logit of the wave, and the sum relative to it (every lane has both).  Relative to the largest of the first vectors, the sum
+    // is taken while the others arrive; where that is 2^-40 of the sum, or nothing, relative to the largest of all, in two more passes.
+    // us with the largest first and so: 1024 x 128256 fp32 272, 242, x 152064 bf16 151, 144; 2048 x 10000 fp16 23.5, 22.0.
     __device__ __forceinline__ Sum wave_sum_of(Temperature t) const
     {
-        float most = edge_z;
-        auto more = [&](uint4v a) {
+        auto larger = [&](float most, uint4v a) {
 #pragma unroll
             for (int e = 0; e < PER; e += 2) most = max3(most, element<DT>(a, e), element<DT>(a, e + 1));
+            return most;
         };
+        auto sum = [&](float base) {
+            float a0 = 0.f, a1 = 0.f;
+            auto add = [&](uint4v a) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) more(kept(i));
-        for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) more(vector(i));
+                for (int e = 0; e < PER; e += 2) {
+                    a0 += exp_logit<DT>(element<DT>(a, e), base, t);
+                    a1 += exp_logit<DT>(element<DT>(a, e + 1), base, t);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < NV; ++i) add(kept(i));
+            for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) add(vector(i));
+            a0 += exp_logit<DT>(edge_z, base, t);
+            return wave_sum(a0 + a1);
+        };
+        const float near_most = wave_max(larger(kNothing, kept(0)));
+        if (near_most != kNothing) {
+            const float total = sum(near_most);
+            if (total < 0x1p40f) return {near_most, total};           // all lanes alike; not with a NaN either
+        }
+        float most = edge_z;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) most = larger(most, kept(i));
+        for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) most = larger(most, vector(i));
         most = wave_max(most);
-        const float base = most == kNothing ? 0.f : most;
-        float a0 = exp_logit<DT>(edge_z, base, t), a1 = 0.f;
-        auto add = [&](uint4v a) {
-#pragma unroll
-            for (int e = 0; e < PER; e += 2) {
-                a0 += exp_logit<DT>(element<DT>(a, e), base, t);
-                a1 += exp_logit<DT>(element<DT>(a, e + 1), base, t);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < NV; ++i) add(kept(i));
-        for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) add(vector(i));
-        return {most, wave_sum(a0 + a1)};
+        return {most, sum(most == kNothing ? 0.f : most)};
     }
 
     // grad = factor exp((z - most) / tau), or zeros

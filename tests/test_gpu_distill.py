@@ -171,3 +171,17 @@ def test_rows_longer_than_what_is_kept(T, V, dtype):
     weight = torch.rand(T, generator=g).to(DEV)
     weight[::7] = 0
     check(logits, ids, top, weight, 1.3, 2.0, f"{T}x{V} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("peak", [5.0, 20.0, 27.0, 29.0, 60.0, 500.0])
+def test_words_far_above_the_others(peak, dtype):
+    """A word e^peak above the rest, at every place that a wave may meet it first or last; some of them stand before masked words."""
+    T, V = 48, 12345
+    logits, ids, top, g = make(T, V, 8, dtype, int(peak), scale=0.3)
+    at = torch.linspace(0, V - 1, T).long()
+    logits[torch.arange(T), at] = peak
+    logits[::4, :4096] = float("-inf")
+    ids[:, 0] = at.to(torch.int32).to(DEV)
+    top[logits.gather(1, ids.long()).isinf()] = float("-inf")
+    check(logits, ids, top, None, 1.0, 1.0, f"peak {peak} {dtype}")
