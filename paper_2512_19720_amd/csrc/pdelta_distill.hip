@@ -223,12 +223,14 @@ struct Words {
     int some;
 };
 
-// p_j of the row's words in LDS; z_of(j, id): the student's logit of word j.
+// p_j of the row's words in LDS; z_of(j, id): the student's logit of word j.  A NaN or +inf among the teacher's logits makes all of its
+// shares NaN, and with them the loss and the gradient's entries of the words.
 template <typename Z>
 __device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, Words& words, Z z_of)
 {
     const int lane = threadIdx.x & 63;
     float best = kNothing;
+    bool mine = false;
     for (int j = lane; j < g.k; j += kWave) {
         int id = g.ids[row * g.k + j];
         float t = kNothing, z = 0.f;
@@ -240,9 +242,10 @@ __device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, Words
         words.share[j] = t;
         words.z[j] = z;
         best = fmaxf(best, t);
+        mine = mine || t != kNothing;
     }
     best = wave_max(best);
-    const bool some = best != kNothing;
+    const bool some = __ballot(mine) != 0;
     float mass = 0.f;
     for (int j = lane; j < g.k; j += kWave) mass += words.id[j] >= 0 ? exp_tau(words.share[j] - best, g.tau) : 0.f;
     mass = wave_sum(mass);
@@ -250,7 +253,7 @@ __device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, Words
     for (int j = lane; j < g.k; j += kWave) {
         const float t = words.share[j], p = words.id[j] >= 0 ? exp_tau(t - best, g.tau) / mass : 0.f;
         words.share[j] = p;
-        if (!(p > 0.f)) words.id[j] = -1;
+        if (p == 0.f) words.id[j] = -1;               // (a share that is not a number keeps its word)
         words.gap[j] = (t - best) / g.tau.tau - log_mass;
     }
     if (lane == 0) words.some = some;
