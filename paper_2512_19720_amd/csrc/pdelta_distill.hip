@@ -72,6 +72,13 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b)
         return f32_to_f16_bits(a) | f32_to_f16_bits(b) << 16;
     }
 }
+// One entry, with the conversion of the vectors: a NaN of any pattern stays one.
+template <int DT>
+__device__ __forceinline__ void store_entry(void* p, int64_t at, float x)
+{
+    if constexpr (DT == kF32) ((float*)p)[at] = x;
+    else ((uint16_t*)p)[at] = (uint16_t)pack_pair<DT>(x, 0.f);
+}
 // The largest of three; none of them is a NaN that signals.
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -195,7 +202,7 @@ struct RowPart {
         for (int i = 0; i < NV; ++i)
             if ((int64_t)i * THREADS + threadIdx.x < vectors) put(i, kept(i));
         for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) put(i, ZERO ? (uint4v){0, 0, 0, 0} : vector(i));
-        if (edge >= 0) store_y<DT>(dst, edge, value(edge_z));
+        if (edge >= 0) store_entry<DT>(dst, edge, value(edge_z));
     }
 };
 
@@ -285,7 +292,7 @@ __device__ __forceinline__ void store_words(const DistillArgs& g, int64_t row, c
         float sum = 0.f;
         for (int i = 0; i < g.k; ++i) sum += words.id[i] == id ? words.share[i] : 0.f;
         const float q = q_factor * exp_logit<DT>(words.z[j], most, g.tau);
-        store_y<DT>(g.grad, row * g.V + id, q - factor * sum);
+        store_entry<DT>(g.grad, row * g.V + id, q - factor * sum);
     }
 }
 

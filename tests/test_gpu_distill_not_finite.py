@@ -60,3 +60,13 @@ def test_a_teachers_logit_that_is_no_number(T, V, k, dtype):
         plain[:, -1] = NAN
         loss, grad = every_form(logits, unused, plain)
         assert loss.isfinite().all() and grad.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("bits", [0x7FFFFFFF, -1, 0x7FC00000, 0x7F800001])
+def test_a_teachers_nan_of_any_pattern(bits, dtype):
+    logits, ids, top = make(3, 501, 4, dtype, 2)
+    top = top.float()
+    top.view(torch.int32)[1, 2] = bits
+    loss, grad = every_form(logits, ids, top)
+    assert loss[1].isnan() and grad[1, ids[1].long()].isnan().all() and loss[[0, 2]].isfinite().all() and grad[[0, 2]].isfinite().all()
