@@ -94,12 +94,13 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-// A large logit and the sum of exponentials relative to it; (-inf, 0) is nothing.
+// A large logit and the sum of exponentials relative to it; (-inf, 0) is nothing.  A logit that is NaN or +inf makes the sum NaN, which
+// no joining takes out again, and with it the loss and the row of the gradient.
 struct Sum { float most, total; };
 __device__ __forceinline__ Sum join(Sum a, Sum b, Temperature t)
 {
     const float most = fmaxf(a.most, b.most);
-    if (most == kNothing) return {kNothing, 0.f};
+    if (most == kNothing) return {kNothing, a.total + b.total};       // 0, or not a number
     return {most, a.total * exp_tau(a.most - most, t) + b.total * exp_tau(b.most - most, t)};
 }
 
@@ -270,11 +271,11 @@ __device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, Words
 __device__ __forceinline__ void write_loss(const DistillArgs& g, int64_t row, const Words& words, Sum all, float w)
 {
     const int lane = threadIdx.x & 63;
-    const float log_total = all.total > 0.f ? logf(all.total) : 0.f;
+    const float log_total = all.total == 0.f ? 0.f : logf(all.total);
     float kl = 0.f;
     for (int j = lane; j < g.k; j += kWave)
         if (words.id[j] >= 0) {
-            const float log_q = all.total > 0.f ? (words.z[j] - all.most) / g.tau.tau - log_total : kNothing;
+            const float log_q = all.total == 0.f ? kNothing : (words.z[j] - all.most) / g.tau.tau - log_total;
             kl += words.share[j] * (words.gap[j] - log_q);
         }
     kl = wave_sum(kl);
@@ -329,7 +330,7 @@ distill_kernel(DistillArgs g)
     if (all.most == kNothing) all.most = 0.f;         // nothing may be answered: every q is 0
     if (wave == 0) write_loss(g, row, words, all, w);
     if (g.grad == nullptr) return;
-    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total > 0.f ? factor / all.total : 0.f;
+    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total != 0.f ? factor / all.total : 0.f;
     part.template store<false>(q_factor, all.most, g.tau);
     __syncthreads();
     store_words<DT>(g, row, words, q_factor, factor, all.most, 0, g.V);
@@ -406,7 +407,7 @@ distill_join_kernel(DistillArgs g, int groups)
     }
     if (g.grad == nullptr) return;
     __syncthreads();
-    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total > 0.f ? factor / all.total : 0.f;
+    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total != 0.f ? factor / all.total : 0.f;
     p.template store<false>(q_factor, all.most, g.tau);
     __syncthreads();
     store_words<DT>(g, row, words, q_factor, factor, all.most, begin, end);

@@ -70,3 +70,25 @@ def test_a_teachers_nan_of_any_pattern(bits, dtype):
     top.view(torch.int32)[1, 2] = bits
     loss, grad = every_form(logits, ids, top)
     assert loss[1].isnan() and grad[1, ids[1].long()].isnan().all() and loss[[0, 2]].isfinite().all() and grad[[0, 2]].isfinite().all()
+
+
+@pytest.mark.parametrize("T,V,k,dtype", SIZES)
+def test_a_students_logit_that_is_no_number(T, V, k, dtype):
+    """softmax over the vocabulary is NaN for every word: the loss is, and the row of the gradient."""
+    logits, ids, top = make(T, V, k, dtype, V + 1)
+    clean_loss, clean_grad = every_form(logits, ids, top)
+    for bad in (NAN, INF):
+        for at in (0, 1, V // 2, V - 1, slice(V // 3, V // 3 + 9), slice(None)):
+            wrong = logits.clone()
+            wrong[1, at] = bad
+            loss, grad = every_form(wrong, ids, top)
+            assert loss[1].isnan() and grad[1].isnan().all(), (bad, at)
+            others_alike(loss, clean_loss, [1])
+            others_alike(grad, clean_grad, [1])
+        # nothing else may be answered
+        wrong = logits.clone()
+        wrong[1] = -INF
+        wrong[1, 2 * V // 3] = bad
+        loss, grad = every_form(wrong, ids, top)
+        assert loss[1].isnan() and grad[1].isnan().all(), bad
+        others_alike(grad, clean_grad, [1])
