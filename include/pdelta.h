@@ -478,9 +478,11 @@ int pdelta_grad_v_experts(const void* X, const void* dY, const int32_t* offsets,
  *   weight      in   fp32 [T], or NULL for 1; a token of weight 0 gives zeros, whatever its logits are
  *   loss        out  fp32 [T]
  *   grad        out  [T, V], dtype; may be the same pointer as logits (the gradient replaces them); NULL: the loss alone
- * A token without a slot in use has loss 0 and gradient 0.  Where p > 0 meets a masked word the loss is +inf and the gradient
- * finite.  A NaN or +inf in a slot in use makes p NaN: the loss of the token and its gradient at the words of its slots are NaN, its
- * other entries are as they would be.  A NaN or +inf among the logits of a token makes its loss and its row of the gradient NaN.  All arithmetic is in fp32; grad is rounded once.  k is 1 .. 1024, V at most 2^22, temperature 10^-6 .. 10^6.
+ * A token without a slot in use, or with shares of 0 only, has loss 0 and gradient 0, whatever its logits are.  Where p > 0 meets a
+ * masked word the loss is +inf and the gradient finite.  A NaN or +inf in a slot in use makes p NaN: the loss of the token and its
+ * gradient at the words of its slots are NaN, its other entries are as they would be.  A NaN or +inf among the logits of a token makes
+ * its loss and its row of the gradient NaN.  All arithmetic is in fp32; grad is rounded once.  k is 1 .. 1024, V at most 2^22,
+ * temperature 10^-6 .. 10^6.
  * T = 0 is a no-op.  workspace as above.
  */
 size_t pdelta_distill_workspace_bytes(int64_t T, int64_t V, int64_t k, int dtype);

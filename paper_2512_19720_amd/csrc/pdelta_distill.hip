@@ -228,7 +228,7 @@ struct Words {
     int id[kDistillMaxWords];                         // -1: no share
     float share[kDistillMaxWords], gap[kDistillMaxWords];         // p, and log p - z / tau
     float wave_most[16], wave_total[16], z[kDistillMaxWords];
-    int some;
+    int some;                                         // a slot is in use
 };
 
 // p_j of the row's words in LDS; z_of(j, id): the student's logit of word j.  A NaN or +inf among the teacher's logits makes all of its
@@ -279,7 +279,7 @@ __device__ __forceinline__ void write_loss(const DistillArgs& g, int64_t row, co
             kl += words.share[j] * (words.gap[j] - log_q);
         }
     kl = wave_sum(kl);
-    if (lane == 0) g.loss[row] = g.tau.tau * g.tau.tau * w * kl;
+    if (lane == 0) g.loss[row] = words.some ? g.tau.tau * g.tau.tau * w * kl : 0.f;
 }
 
 // The entries of the words in [begin, end): a word that is named more than once gets all its shares, from each of its threads.
@@ -330,7 +330,11 @@ distill_kernel(DistillArgs g)
     if (all.most == kNothing) all.most = 0.f;         // nothing may be answered: every q is 0
     if (wave == 0) write_loss(g, row, words, all, w);
     if (g.grad == nullptr) return;
-    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total != 0.f ? factor / all.total : 0.f;
+    if (!words.some) {                                // whole workgroup; the row's logits do not matter here either
+        part.template store<true>(0.f, 0.f, g.tau);
+        return;
+    }
+    const float factor = g.grad_scale * g.tau.tau * w, q_factor = all.total != 0.f ? factor / all.total : 0.f;
     part.template store<false>(q_factor, all.most, g.tau);
     __syncthreads();
     store_words<DT>(g, row, words, q_factor, factor, all.most, 0, g.V);
@@ -407,7 +411,11 @@ distill_join_kernel(DistillArgs g, int groups)
     }
     if (g.grad == nullptr) return;
     __syncthreads();
-    const float factor = g.grad_scale * g.tau.tau * w, q_factor = words.some && all.total != 0.f ? factor / all.total : 0.f;
+    if (!words.some) {                                // whole workgroup
+        p.template store<true>(0.f, 0.f, g.tau);
+        return;
+    }
+    const float factor = g.grad_scale * g.tau.tau * w, q_factor = all.total != 0.f ? factor / all.total : 0.f;
     p.template store<false>(q_factor, all.most, g.tau);
     __syncthreads();
     store_words<DT>(g, row, words, q_factor, factor, all.most, begin, end);

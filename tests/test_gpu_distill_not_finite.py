@@ -92,3 +92,22 @@ def test_a_students_logit_that_is_no_number(T, V, k, dtype):
         loss, grad = every_form(wrong, ids, top)
         assert loss[1].isnan() and grad[1].isnan().all(), bad
         others_alike(grad, clean_grad, [1])
+
+
+@pytest.mark.parametrize("T,V,k,dtype", SIZES)
+def test_a_token_without_a_slot_in_use(T, V, k, dtype):
+    """Loss and gradient are 0 whatever the token's logits hold: the rows of padding of a batch."""
+    logits, ids, top = make(T, V, k, dtype, V + 2)
+    clean_loss, clean_grad = every_form(logits, ids, top)
+    ids[1] = -1
+    for row in (1, 0):
+        if row == 0:
+            top[0] = -INF                             # slots, but no share
+        for bad in (NAN, INF, -INF):
+            for at in (V // 2, slice(None)):
+                wrong = logits.clone()
+                wrong[row, at] = bad
+                loss, grad = every_form(wrong, ids, top)
+                assert float(loss[row]) == 0 and not grad[row].any(), (row, bad, at)
+                others_alike(loss, clean_loss, [0, 1])
+                others_alike(grad, clean_grad, [0, 1])
