@@ -2,16 +2,16 @@
 // q = softmax(z) over the vocabulary and p = softmax(top / tau) over the teacher's words that are in use:
 //   loss    = tau^2 w sum_j p_j (log p_j - log q[id_j])
 //   grad[i] = scale tau w (q[i] - sum_{j: id_j = i} p_j)
-// All of it is in fp32; sums over the vocabulary are taken relative to a large logit.
+// All of it is in fp32; sums over the vocabulary are taken relative to the largest logit.
 //
 // Bound by memory: logits once in, gradient once out (2048 x 128256 bf16, three tenths of the tokens without weight, 193 us: 0.38 GB read
 // and 0.53 written, 4.7 TB/s; a copy of 1 GiB reaches 5.2.  The loss alone of 640 x 32000 fp16 in 13 us: the launch, and 2.5 rows for
 // each CU).  A workgroup keeps its part of the row in registers, as the 16-byte vectors it was loaded as, between the sum over the
-// vocabulary and the gradient; what does not fit is read again.  Every wave sums relative to a large logit of its own, and the
+// vocabulary and the gradient; what does not fit is read again.  Every wave sums relative to the largest logit of its own, and the
 // waves meet once; the first wave deals with the teacher's words meanwhile.  The gradient is written as if the teacher had named no
 // word, and the words' own entries again after a barrier.
 //
-// Of few tokens, a long row is split among workgroups: one launch leaves a large logit and the sum of every part (and the
+// Of few tokens, a long row is split among workgroups: one launch leaves the largest logit and the sum of every part (and the
 // words' logits, since the gradient may replace the logits) in the workspace, a second one joins them in their order.
 #include <algorithm>
 #include <cmath>
@@ -23,6 +23,7 @@ namespace pdelta {
 
 constexpr int kDistillMaxWords = 1024;
 constexpr float kNothing = -INFINITY;
+constexpr float kNear = 8.f;                          // RowPart::wave_sum_of
 
 // exp(x / tau) is 2^(x hi + x lo) with log2(e) / tau = hi + lo; hi is below the quotient and lo above 0, so that with x = -inf
 // both products are -inf.  16-bit logits are taken with `near`, the quotient itself in fp32: the rounding of that factor, 2^-25
@@ -94,7 +95,7 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-// A large logit and the sum of exponentials relative to it; (-inf, 0) is nothing.  A logit that is NaN or +inf makes the sum NaN, which
+// The largest logit and the sum of exponentials relative to it; (-inf, 0) is nothing.  A logit that is NaN or +inf makes the sum NaN, which
 // no joining takes out again, and with it the loss and the row of the gradient.
 struct Sum { float most, total; };
 __device__ __forceinline__ Sum join(Sum a, Sum b, Temperature t)
@@ -144,9 +145,11 @@ struct RowPart {
     __device__ __forceinline__ int64_t place(int64_t i) const { return (first + (i * THREADS + threadIdx.x) * PER) * (DT == kF32 ? 4 : 2); }
     __device__ __forceinline__ uint4v vector(int64_t i) const { return *(const uint4v*)(src + place(i)); }
 
-    // A large logit of the wave, and the sum relative to it (every lane has both).  Relative to the largest of the first vectors, the sum
-    // is taken while the others arrive; where that is 2^-40 of the sum, or nothing, relative to the largest of all, in two more passes.
-    // us with the largest first and so: 1024 x 128256 fp32 272, 242, x 152064 bf16 151, 144; 2048 x 10000 fp16 23.5, 22.0.
+    // The wave's largest logit, and the sum relative to it (every lane has both).  The sum is taken while the vectors arrive, relative to the
+    // largest of the first ones; the same pass finds the largest of all, and one factor brings the sum to it.  Where that is more than
+    // kNear powers of two above (a word that stands out), or the first ones are all masked, the sum is taken again relative to it:
+    // a logit far above makes the arguments of the exponentials large, and their rounding is most of what is left of 1 - q and log q.
+    // us with the largest first, in a pass of its own, and so: 1024 x 128256 fp32 272, 242, x 152064 bf16 151, 144; 2048 x 10000 fp16 23.5, 22.1.
     __device__ __forceinline__ Sum wave_sum_of(Temperature t) const
     {
         auto larger = [&](float most, uint4v a) {
@@ -154,13 +157,16 @@ struct RowPart {
             for (int e = 0; e < PER; e += 2) most = max3(most, element<DT>(a, e), element<DT>(a, e + 1));
             return most;
         };
-        auto sum = [&](float base) {
+        auto sum = [&](float base, auto each) {
             float a0 = 0.f, a1 = 0.f;
             auto add = [&](uint4v a) {
 #pragma unroll
                 for (int e = 0; e < PER; e += 2) {
-                    a0 += exp_logit<DT>(element<DT>(a, e), base, t);
-                    a1 += exp_logit<DT>(element<DT>(a, e + 1), base, t);
+                    const float x = element<DT>(a, e), y = element<DT>(a, e + 1);
+                    each(x, y);
+                    a0 += exp_logit<DT>(x, base, t);
+                    a1 += exp_logit<DT>(y, base, t);
+                    __builtin_amdgcn_sched_barrier(0);             // (else 6 registers more, and fewer waves on a CU: 2048 x 70001 bf16 145 us, 124)
                 }
             };
 #pragma unroll
@@ -170,16 +176,18 @@ struct RowPart {
             return wave_sum(a0 + a1);
         };
         const float near_most = wave_max(larger(kNothing, kept(0)));
-        if (near_most != kNothing) {
-            const float total = sum(near_most);
-            if (total < 0x1p40f) return {near_most, total};           // all lanes alike; not with a NaN either
-        }
         float most = edge_z;
+        if (near_most != kNothing) {
+            const float total = sum(near_most, [&](float x, float y) { most = max3(most, x, y); });
+            most = wave_max(most);
+            if ((most - near_most) * t.near <= kNear) return {most, total * exp_logit<DT>(near_most, most, t)};       // all lanes alike
+        } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) most = larger(most, kept(i));
-        for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) most = larger(most, vector(i));
-        most = wave_max(most);
-        return {most, sum(most == kNothing ? 0.f : most)};
+            for (int i = 0; i < NV; ++i) most = larger(most, kept(i));
+            for (int64_t i = NV; i * THREADS + threadIdx.x < vectors; ++i) most = larger(most, vector(i));
+            most = wave_max(most);
+        }
+        return {most, sum(most == kNothing ? 0.f : most, [](float, float) {})};
     }
 
     // grad = factor exp((z - most) / tau), or zeros
