@@ -126,7 +126,7 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
     float* red = (float*)(grad_smem + 2 * kGradStage + 8192);         // [2][256]
 
     float16v acc[FP][FQ];
-    float sum[FQ] = {0.f, 0.f};
+    float sum[FQ] = {0.f, 0.f}, tile_sum[FQ];         // of the run, and of one of its tiles: 64 additions, then one for each tile
 
     // this lane's part of a transposing read: token (lane / 32) * 8 + lane % 16 / 4, columns (lane / 16 % 2) * 16 + lane % 4 * 4; 32
     // columns further is 64 bytes, exclusive or with the place's own bits
@@ -158,9 +158,11 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
     // 32x32 accumulator: element r of lane l is row (r/4)*8 + (l/32)*4 + r%4, column l%32
     auto add = [&](int h, float x, uint32_t word, int left) {     // +-x by the bit that `left` brings to the top
         const uint32_t one = ((word << left) & 0x80000000u) ^ 0xBF800000u;
-        sum[h] = __builtin_fmaf(x, __builtin_bit_cast(float, one), sum[h]);
+        tile_sum[h] = __builtin_fmaf(x, __builtin_bit_cast(float, one), tile_sum[h]);
     };
     auto add_tile = [&]() {
+#pragma unroll
+        for (int h = 0; h < FQ; ++h) tile_sum[h] = 0.f;
         if constexpr (AXIS == 0) {
 #pragma unroll
             for (int f = 0; f < FP; ++f)
@@ -187,6 +189,8 @@ experts_grad_kernel(const uint16_t* __restrict__ X, int x_ld, const uint16_t* __
                 __builtin_amdgcn_sched_barrier(0);    // (else all of the words are read at once, into registers that are not there)
             }
         }
+#pragma unroll
+        for (int h = 0; h < FQ; ++h) sum[h] += tile_sum[h];
     };
 
     // Step `now` of all the tiles' steps, step s of its tile.  The barrier is three quarters into it: by then every wave has read its
