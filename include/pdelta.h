@@ -422,8 +422,9 @@ int pdelta_patch_group(const void* W_b, const uint32_t* B_packed, const uint16_t
  * Arithmetic: weights as in pdelta_linear_row for M > 64 (one rounding of W_hat to fp16, fp32 sums, one rounding of Y); bf16
  * tokens are multiplied as fp16 after scaling every row by a power of two, so that X has no range to stay in (elements
  * below 2^-28 of the largest of their row lose low bits); bf16 weights must stay below 65504 in magnitude.  With few tokens,
- * M at most 16 (bf16: 32) times the smaller of E and M, and d_in a multiple of 128, as in pdelta_linear_row / _col for
- * M <= 64 instead: two accumulators in the operands' own format, in column mode with fp16(X v) as the sign part's operand.
+ * M at most 16 times n, the smaller of E and M (32 times where n times d_out / 256, rounded up, is at most 128), and d_in a multiple
+ * of 128, as in pdelta_linear_row / _col for M <= 64 instead: two accumulators in the operands' own format, in column mode with
+ * fp16(X v) as the sign part's operand.
  */
 size_t pdelta_linear_experts_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int x_dtype);
 

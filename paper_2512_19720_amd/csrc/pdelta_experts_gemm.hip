@@ -142,7 +142,7 @@ static int launch_product(const ExpertsCall& call, bool grad, hipStream_t stream
 
 size_t experts_linear_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
 {
-    if (M == 0 || experts_decode_tokens(M, E, d_in, dtype) > 0) return 0;
+    if (M == 0 || experts_decode_tokens(M, E, d_out, d_in) > 0) return 0;
     return ProductLayout(false, M, E, d_out, d_in, dtype).all;
 }
 size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64_t d_in, int dtype)
@@ -151,7 +151,7 @@ size_t experts_grad_x_workspace_bytes(int64_t M, int64_t E, int64_t d_out, int64
 }
 int launch_experts_linear(const ExpertsCall& c, hipStream_t stream)
 {
-    const int mt = experts_decode_tokens(c.M, c.E, c.d_in, c.dtype);
+    const int mt = experts_decode_tokens(c.M, c.E, c.d_out, c.d_in);
     return mt > 0 ? launch_experts_skinny(c, mt, stream) : launch_product(c, false, stream);
 }
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream) { return launch_product(c, true, stream); }

@@ -47,15 +47,20 @@ static int launch_skinny(const ExpertsCall& c, hipStream_t stream)
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
-// Up to 16 tokens for each expert that can be met, always; up to 32 of bf16 (the tiles of 256 outputs convert their weights).
-// Uneven experts read their weights once for each 16 (32) of their tokens.  us here and on those tiles, experts x outputs x inputs,
-// bf16 row: 32 x 2048 x 4096, 10 tokens each 99 and 131, 24 120 and 140, 32 130 and 133; 8 x 4096 x 4096 10 43 and 64, 24 60 and 65;
-// 4 x 11008 x 4096 10 67 and 81, 24 96 and 83; fp16 col: 32 x 2048 x 4096 10 101 and 125, 24 137 and 128.
-int experts_decode_tokens(int64_t M, int64_t E, int64_t d_in, int dtype)
+// Up to 16 tokens for each expert that can be met, always; up to 32 where those experts have at most 128 tiles of 256 outputs, half a
+// tile for each CU: with more of them the large tiles fill the CUs, and with fewer they are cut into parts and summed by another launch.
+// Uneven experts read their weights once for each 16 (32) of their tokens.  us here and on the large tiles, experts x outputs x inputs, bf16 row:
+// 32 x 2048 x 4096, 10 tokens each 99 and 131; 4 x 11008 x 4096 10 67 and 81.  Of 17 to 32 tokens each, over nine layers of 256 x 512 to
+// 14336 x 4096, 1 to 64 experts, even and uneven, both types and kinds of scales: time over the better of the two 1.026 on average with this
+// limit (geometric mean; own bases 1.022, one base 1.031), 1.067 always here, 1.38 always there.  fp16 row, 20 tokens each: 4 x 4096 x 4096
+// (64 tiles) 34.7 and 36.7, with one base 18.0 and 36.4; 8 x 4096 x 4096 (128) 65.8 and 61.1, with one base 31.7 and 57.4.  What the limit
+// gets wrong most: two uneven experts of 14336 x 4096 (112), fp16 column, 1.6 times the large tiles' time; 32 of 1408 x 2048 with one base (192), bf16 row,
+// 1.7 times the time here.
+int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in)
 {
     if (M == 0 || d_in % kDmaUnitK != 0) return 0;
     const int64_t met = std::min(E, M), each = (M + met - 1) / met;
-    return each <= 16 ? 1 : each <= 32 && dtype == kBF16 ? 2 : 0;
+    return each <= 16 ? 1 : each <= 32 && met * ((d_out + 255) / 256) <= 128 ? 2 : 0;
 }
 
 int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream)

@@ -155,7 +155,7 @@ int launch_experts_linear(const ExpertsCall& c, hipStream_t stream);
 int launch_experts_grad_x(const ExpertsCall& c, hipStream_t stream);
 
 // The forward product where experts have few tokens, 16 mt at a time.  experts_decode_tokens: that mt, or 0 for the tiles below.
-int experts_decode_tokens(int64_t M, int64_t E, int64_t d_in, int dtype);
+int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in);
 int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream);
 
 // The products on tiles of 256 outputs with direct loads: A holds fp16 rows of lda values, a multiple of 128; inverse: a factor for
