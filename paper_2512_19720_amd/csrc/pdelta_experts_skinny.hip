@@ -65,9 +65,13 @@ int experts_decode_tokens(int64_t M, int64_t E, int64_t d_out, int64_t d_in)
 
 int launch_experts_skinny(const ExpertsCall& c, int mt, hipStream_t stream)
 {
-    // One row tile for a workgroup where it has a while to read (10 tokens for each of 32 experts, 2048 x 4096 bf16: 99 us, 120 with
-    // two), two for short rows (64 experts, 1408 x 2048: 82 and 70).
-    const bool one = c.d_in > 2048;
+    // Two row tiles for a workgroup, which share the loads of the tokens.  One where the rows of W_b are a multiple of 8 KB apart, so that the
+    // same inputs of 32 rows lie in few of the memory's channels, and come from there: not out of the caches, where one base of up to 64 MB
+    // stays.  us with one and two, 10 tokens each, bf16 row, experts x outputs x inputs: 16 x 2048 x 4096 51.8, 65.1, x 3584 39.0, 37.3, x 5120 67.9,
+    // 63.6; 32 x 1408 x 2048 40.9, 38.4; one base: 16 x 4096 x 4096 58.9, 46.7, 4 x 14336 x 4096 76.5, 91.7, 8 x 4096 x 8192 87.1, 60.3.  Over 25 layers of
+    // 256 x 512 to 28672 x 1024, 1 to 64 experts of 1 to 16 tokens: time over the better one's 1.007 on average (geometric mean), 1.15 with one, 1.04
+    // with two.
+    const bool one = c.d_in % 4096 == 0 && (c.w_stride != 0 || c.d_out * c.d_in > 1 << 25);
 #define PDELTA_GO(XDT, AXIS)                                              \
     {                                                                     \
         if (mt == 2) return launch_skinny<XDT, AXIS, 2, 2>(c, stream);    \
