@@ -204,7 +204,7 @@ struct RowPart {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) r[p] = pack_pair<DT>(value(element<DT>(a, 2 * p)), value(element<DT>(a, 2 * p + 1)));
             }
-            // (not to be kept in the caches: us otherwise and so, 2048 x 128256 bf16 238, 227, x 70001 143, 125, 1024 x 128256 fp32 293, 263)
+            // (not to be kept in the caches: us otherwise and so, 2048 x 128256 bf16 235, 227, x 70001 141, 125, 1024 x 128256 fp32 269, 248)
             __builtin_nontemporal_store(r, (uint4v*)(dst + place(i)));
         };
 #pragma unroll
@@ -429,9 +429,9 @@ distill_join_kernel(DistillArgs g, int groups)
     store_words<DT>(g, row, words, q_factor, factor, all.most, begin, end);
 }
 
-// Parts of a row: of few tokens, rows of more than 128 KB are split into parts of 32 KB.  us in one part, 4, 8 and 16: 1 x 128256 bf16
-// 18.5, 16.0, 11.7 and 12.4, 64 tokens 21.1, 19.6, 15.7 and 19.0, 150 tokens 24.3, 30.3, 26.3 and 33.7; 16 x 128256 fp32 24.0, 23.5, 16.2
-// and 12.9; but 3 x 32001 fp32 (125 KB) 9.2, 10.6, 10.8 and 10.7.
+// Parts of a row: of few tokens, rows of more than 128 KB are split into parts of 32 KB.  us of a call in one part, 4, 8 and 16: 1 x 128256
+// bf16 21.7, 18.1, 15.2 and 15.1, 64 tokens 22.4, 21.7, 17.9 and 21.0, 150 tokens 24.8, 30.6, 28.1 and 35.9; 16 x 128256 fp32 26.5, 27.8, 18.8
+// and 15.8; but 3 x 32001 fp32 (125 KB) 9.2, 13.9, 14.3 and 14.1.
 static int row_parts(int64_t T, int64_t V, int dtype)
 {
     const int64_t bytes = V * (dtype == kF32 ? 4 : 2);
@@ -465,17 +465,17 @@ static int launch_rows(const DistillCall& c, hipStream_t stream)
         hipLaunchKernelGGL(distill_join_kernel<DT>, dim3((unsigned)(c.T * groups)), dim3(256), 0, stream, g, groups);
     } else {
         // Threads and the 16-byte vectors that each keeps in registers.  Eight let twice as many waves run on a CU as sixteen, for which the
-        // rest of a row that is a little too long is read again.  us with sixteen and eight, 16-bit: 8192 x 10000 97, 75, the loss
-        // alone 69, 43; 2048 x 82000 172, 153, x 90000 185, 172, x 100000 192, 194, x 128256 227, 257; the loss alone of 70000 111, 63.
-        // 32000 in 512 threads of eight: 217, sixteen in 256 221, and 10000 107, 97.  The loss alone takes what the gradient would: its bits
-        // are the same.
+        // rest of a row that is too long is read again.  us with sixteen and eight, 16-bit: 8192 x 10000 94, 69, the loss
+        // alone 65, 43; 2048 x 82000 173, 149, x 100000 207, 187, x 120000 223, 215, x 128256 227, 230; the loss alone of 70000 100, 56.  fp32:
+        // 2048 x 46000 161, 163, x 57000 206, 216, the loss alone 94, 80 and 107, 98.  8192 x 32000 in 512 threads of eight 205, in 256 of sixteen
+        // 208.  The loss alone takes what the gradient would: its bits are the same.
         const int64_t vectors = c.V / PER;
 #define PDELTA_GO(THREADS, NV) hipLaunchKernelGGL((distill_kernel<DT, THREADS, NV>), dim3((unsigned)c.T), dim3(THREADS), 0, stream, g)
         if (vectors <= 256) PDELTA_GO(256, 1);
         else if (vectors <= 4 * 256) PDELTA_GO(256, 4);
         else if (vectors <= 8 * 256) PDELTA_GO(256, 8);
         else if (vectors <= 16 * 256) PDELTA_GO(256, 16);
-        else if (vectors <= 12 * 1024) PDELTA_GO(1024, 8);
+        else if (vectors <= (DT == kF32 ? 12 : 15) * 1024) PDELTA_GO(1024, 8);
         else PDELTA_GO(1024, 16);
 #undef PDELTA_GO
     }

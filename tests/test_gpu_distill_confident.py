@@ -13,6 +13,7 @@ import torch
 
 from experts_util import U, half_step
 from paper_2512_19720_amd import binding as pd
+from test_gpu_distill import check, make
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -42,3 +43,13 @@ def test_a_student_that_is_sure(T, V, dtype):
     bound = bound + (want.abs() + bound) * rel + least
     off = (grad[rows, at].double() - want).abs()
     assert bool((off <= bound).all()), float((off / bound).max())
+
+
+@pytest.mark.parametrize("T,V,dtype", [(129, 122880, BF16), (130, 122881, F16), (129, 122889, BF16), (129, 49152, F32), (130, 49157, F32)])
+def test_rows_at_the_ends_of_what_is_kept(T, V, dtype):
+    """Rows that end where threads begin to keep more of them; some whose largest logits come last."""
+    logits, ids, top, g = make(T, V, 5, dtype, T + V)
+    logits[1::3, :V - 5] -= 40
+    logits[2::5, :V // 2] = float("-inf")
+    top[logits.gather(1, ids.long()).isinf()] = float("-inf")
+    check(logits, ids, top, None, 0.8, 2.0, f"{T}x{V} {dtype}")
