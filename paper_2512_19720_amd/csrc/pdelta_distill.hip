@@ -4,9 +4,9 @@
 //   grad[i] = scale tau w (q[i] - sum_{j: id_j = i} p_j)
 // All of it is in fp32; sums over the vocabulary are taken relative to the largest logit.
 //
-// Bound by memory: logits once in, gradient once out (2048 x 128256 bf16, three tenths of the tokens without weight, 193 us: 0.38 GB read
-// and 0.53 written, 4.7 TB/s; a copy of 1 GiB reaches 5.2.  The loss alone of 640 x 32000 fp16 in 13 us: the launch, and 2.5 rows for
-// each CU).  A workgroup keeps its part of the row in registers, as the 16-byte vectors it was loaded as, between the sum over the
+// Bound by memory: logits once in, gradient once out (2048 x 128256 bf16, three tenths of the tokens without weight, 195 to 210 us: 0.38 GB
+// read and 0.53 written, 4.3 to 4.7 TB/s; an elementwise copy of 1 GiB reaches 6.2.  The loss alone of 640 x 32000 fp16 in 13 us: the launch, and
+// 2.5 rows for each CU).  A workgroup keeps its part of the row in registers, as the 16-byte vectors it was loaded as, between the sum over the
 // vocabulary and the gradient; what does not fit is read again.  Every wave sums relative to the largest logit of its own, and the
 // waves meet once; the first wave deals with the teacher's words meanwhile.  The gradient is written as if the teacher had named no
 // word, and the words' own entries again after a barrier.

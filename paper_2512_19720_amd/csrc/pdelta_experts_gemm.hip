@@ -2,7 +2,9 @@
 //   forward   Y[m, o]  = sum_i X[m, i]  W_hat_e[o, i]
 //   backward  dX[m, i] = sum_o dY[m, o] W_hat_e[o, i]
 // for the tokens m of every expert e.  The arithmetic is that of the prefill kernels: the tile of W_hat is formed as
-// fp16(W_b +- v) with one rounding, fp32 sums.  This file prepares the operands; the tiles are in pdelta_experts_gemm_dma.hip, and
+// fp16(W_b +- v) with one rounding, fp32 sums.  (That rounding weighs as much as the one of fp16 outputs: 2.9e-4 from the exact products
+// in norm, 2.1e-4 without it; of bf16 outputs 1.67e-3 and 1.66e-3.  W_b and v (.) B as two operands would do without it, for twice the
+// matrix instructions.)  This file prepares the operands; the tiles are in pdelta_experts_gemm_dma.hip, and
 // those of experts with few tokens in pdelta_experts_skinny.hip.
 //
 // The token operand is always multiplied as fp16.  A bf16 one is converted first, by experts_prepare_kernel, every row

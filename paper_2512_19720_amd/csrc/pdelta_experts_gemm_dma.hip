@@ -3,9 +3,9 @@
 // LDS; W_b comes through registers and goes to LDS as W_hat, between the matrix instructions of the step before; one barrier per step,
 // three quarters into it, which publishes step s + 1 and frees the stages of step s.
 //
-// What bounds it: full tiles of one expert (2048 tokens, 8192 x 4096 fp16, one round of 256 tiles) run at 1000 TFLOP/s, 86 % of what a
-// large library product reaches on this card, the matrix cores busy 56 % of the time at clocks that power limits (1.4 to 1.7 GHz).
-// Uneven experts lose more: 2048 tokens x 2 of 8 experts, 14336 x 4096 bf16, 690 TFLOP/s: 8 % of the tiles' rows are no tokens, the
+// What bounds it: full tiles of one expert (2048 tokens, 8192 x 4096 fp16, one round of 256 tiles) take 140 to 147 us, 930 to 980 TFLOP/s, three
+// quarters of what a library product of these sizes reaches (106 us), the matrix cores busy 56 % of the time at clocks that power
+// limits (1.4 to 1.7 GHz).  Uneven experts lose more: 2048 tokens x 2 of 8 experts, 14336 x 4096 bf16, 680 TFLOP/s: 8 % of the tiles' rows are no tokens, the
 // busiest CUs work half a tile longer than the others, and bf16 weights cost 10 % for their conversion (matrix cores 50 % busy).  HBM
 // is not it: 1.8 GB in 700 us.
 //

@@ -3,9 +3,9 @@
 // with the signs:  row  grad[e, o] = sum_i B_e[o, i] D_e[o, i],   col  grad[e, i] = sum_o B_e[o, i] D_e[o, i].
 // D is formed tile by tile on the matrix cores in the operands' own format (exact products, fp32 sums) and never written:
 // the signs meet it in the accumulators, so they are read once for every expert that has tokens, and its few tokens are
-// all that the contraction runs over.  Bound by the matrix cores: 2048 tokens x 2 of 8 experts, 14336 x 4096 bf16 column in 515 us, 930
-// TFLOP/s or 77 % of a large library product, the cores 48 % busy at clocks that power limits; 1.3 GB from memory.  The dimension that is summed over is the accumulator's row dimension, the other one
-// its columns: a lane adds its own elements, and two lanes meet once.
+// all that the contraction runs over.  Bound by the matrix cores: 2048 tokens x 2 of 8 experts, 14336 x 4096 bf16 column in 505 to 540 us, 890
+// to 950 TFLOP/s or 60 % of a large library product, the cores 48 % busy at clocks that power limits; 1.3 GB from memory.  The dimension
+// that is summed over is the accumulator's row dimension, the other one its columns: a lane adds its own elements, and two lanes meet once.
 #include <algorithm>
 
 #include "pdelta_experts.h"
